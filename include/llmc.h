@@ -536,6 +536,122 @@ llmc_status_t llmc_layer_forward_gated(const llmc_layer_desc_t* layer, llmc_bank
                                        size_t workspace_bytes, llmc_stream_t stream);
 size_t llmc_layer_workspace_bytes(const llmc_layer_desc_t* layer, int32_t B, int32_t S, int32_t k);
 
+/* ---- the paged key/value cache of a decoder ------------------------------------------ */
+
+/*
+ * Section V-A compares reuse across inputs with the key/value cache of a decoder (GPT-2): within one sequence the keys and
+ * values of earlier tokens are kept, and only new tokens are computed.  The cache of one layer is a pool of pages:
+ *   d_k, d_v [n_pages, n_kv_heads, page_size, head_dim], element type `dtype`, caller-owned
+ * page_size is a power of two from 16 to 1024, head_dim 64 or 128.
+ */
+typedef struct {
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  int32_t dtype; /* llmc_dtype_t */
+  void *d_k, *d_v;
+} llmc_kv_desc_t;
+
+/*
+ * The sequences of a call.  Slot j of sequence b is place j % page_size of page d_table[b, j / page_size]; its tokens are in
+ * slots 0 .. d_length[b] - 1, and the NEW ones of this call are the last of them (d_length counts them already, before they
+ * are stored).  Their rows are d_new_start[b] .. d_new_start[b + 1] - 1 of the call's row arrays (ascending, within
+ * [0, n_rows)); d_new_start NULL: one new token per sequence, row b (n_rows = n_seqs, max_new = 1).  Rows of no sequence
+ * are neither read nor written.  n_rows may be 0.
+ *   d_table [n_seqs, max_pages], d_length [n_seqs], d_new_start [n_seqs + 1]
+ *   max_new, max_len: bounds, known to the host, of a sequence's new tokens and of d_length (launch sizes and workspaces
+ *          depend on them alone, so a recorded graph serves every state of the tables within them);
+ *          max_len <= max_pages * page_size
+ *   d_pos [n_seqs, max_pages * page_size] or NULL: position (>= 0, below 2^31, increasing from new token to new token) of
+ *          the token in each slot; NULL = the slot's number.  Needed once tokens have been evicted (slots are then no positions).
+ *   d_weight [n_seqs, max_pages * page_size] or NULL: accumulated attention weight of the token in each slot
+ * A page may stand in the tables of several sequences (a shared prefix) as long as no call stores into it or evicts from it;
+ * positions and weights are kept per sequence.  Lengths and chunks are cut to their bounds on the device, and a
+ * page number outside [0, n_pages) is no page: its tokens are not stored, not seen, not moved.
+ */
+typedef struct {
+  int32_t n_seqs, max_pages;
+  const int32_t* d_table;
+  const int32_t* d_length;
+  const int32_t* d_new_start;
+  int32_t n_rows, max_new, max_len;
+  int32_t* d_pos;
+  float* d_weight;
+} llmc_kv_batch_t;
+#define LLMC_MAX_KV_SEQS 65535
+
+/*
+ * Store the keys and values of the new tokens.  d_k_new, d_v_new: row r starts at element r * ld_k (ld_v) and holds
+ * [n_kv_heads, head_dim] of the cache's element type (row strides a multiple of 16 bytes: a slice of a projection's
+ * output will do).  With batch->d_pos the positions are written too (d_pos_new [n_rows], NULL = slot numbers); with
+ * batch->d_weight the new slots' weights become 0.  Copies: exact.
+ * Errors: INVALID_ARG, SHAPE, DTYPE.
+ */
+llmc_status_t llmc_kv_append(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const void* d_k_new, int64_t ld_k,
+                             const void* d_v_new, int64_t ld_v, const int32_t* d_pos_new, llmc_stream_t stream);
+
+/*
+ * The attention of llmc_attention_paged.  Query head h reads key/value head h / (n_heads / n_kv_heads).
+ *   x = scale * <q, k>;  softcap c > 0: x = c * tanh(x / c);  d_slopes [n_heads] fp32: x -= slope_h * (pos_q - pos_k)
+ *   A new token sees the slots up to its own; window w > 0: of these, the ones with pos_q - pos_k < w.
+ */
+typedef struct {
+  int32_t n_heads;
+  float scale;           /* > 0; commonly 1 / sqrt(head_dim) */
+  float softcap;         /* 0 = none */
+  int32_t window;        /* 0 = none */
+  const float* d_slopes; /* or NULL */
+  int32_t accumulate;    /* 1: batch->d_weight[b, j] += the softmax weights of slot j, summed over the new tokens and heads */
+} llmc_attn_desc_t;
+
+/*
+ * Attention of the new tokens (stored beforehand) over their sequences' caches: d_out[r] [n_heads, head_dim] = sum_j p_j v_j,
+ * p = softmax of x over the slots that the token sees; zeros where it sees none.  d_q and d_out: rows ld_q and ld_out elements
+ * apart (multiples of 16 bytes), element type of the cache; d_out must not overlap d_q or the pages.
+ * Softmax statistics, sums and accumulated weights are fp32 in a fixed order (no atomics); with bf16 elements the weights of
+ * the value product are rounded to bf16.  What slots beyond a sequence's length hold does not matter.
+ * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.
+ * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite), SHAPE (head
+ * counts, strides, alignment, bounds), DTYPE, WORKSPACE.
+ */
+llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const llmc_attn_desc_t* attn,
+                                   const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* d_workspace,
+                                   size_t workspace_bytes, llmc_stream_t stream);
+/* sizes only: no pointer of the three structures is read; 0 for sizes that the call refuses */
+size_t llmc_attention_paged_workspace_bytes(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch,
+                                            const llmc_attn_desc_t* attn);
+
+/*
+ * Keep a cache within a budget, by the rule of Section IV-D turned to tokens (what has been used least goes): of every sequence
+ * with d_length[b] > d_keep[b], the tokens that come first by ascending (protected, weight, position, slot) are evicted until
+ * d_keep[b] are left.  Protected are the positions below n_sink and the n_recent highest position numbers of the sequence
+ * (they go last).  A NaN weight ranks above every number.  The kept tokens of slots d_keep[b] and up then move into the slots
+ * that fell free below, the i-th of them into the i-th of those, with their position and weight; slots from the new length on
+ * keep what they held.
+ *   batch: d_pos and d_weight are needed; d_new_start, n_rows and max_new are ignored.  Every page of a sequence that is cut
+ *          must be its own.
+ *   d_keep [n_seqs]; d_length_out [n_seqs] = min(d_length, max(d_keep, 0)) (may be d_length itself)
+ *   d_workspace: at least llmc_kv_evict_workspace_bytes(n_seqs, max_len) bytes, 16-byte aligned
+ * Several layers that share tables and lengths call this once each, with one d_length_out apart from d_length.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, WORKSPACE.
+ */
+llmc_status_t llmc_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const int32_t* d_keep, int32_t n_sink,
+                            int32_t n_recent, int32_t* d_length_out, void* d_workspace, size_t workspace_bytes,
+                            llmc_stream_t stream);
+size_t llmc_kv_evict_workspace_bytes(int32_t n_seqs, int32_t max_len);
+
+/*
+ * The decoder block (arch 1) on new tokens: x1 = x + MHA(LN1(x)), y = x1 + W2 act(W1 LN2(x1) + b1) + b2 for the n_rows rows of
+ * d_h_in [n_rows, d], where the new tokens' keys and values are stored as llmc_kv_append does (positions d_pos_new) and MHA
+ * attends as llmc_attention_paged does.  kv: the layer's element type, n_kv_heads = n_heads, head_dim 64; attn->n_heads =
+ * layer->n_heads.  d_h_out must not overlap d_h_in; its rows of no sequence are undefined.
+ * d_workspace: at least llmc_layer_paged_workspace_bytes(layer, batch, attn) bytes (sizes only), 256-byte aligned.
+ * Errors: as the calls it stands for.
+ */
+llmc_status_t llmc_layer_forward_paged(const llmc_layer_desc_t* layer, const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch,
+                                       const llmc_attn_desc_t* attn, const int32_t* d_pos_new, const void* d_h_in,
+                                       void* d_h_out, void* d_workspace, size_t workspace_bytes, llmc_stream_t stream);
+size_t llmc_layer_paged_workspace_bytes(const llmc_layer_desc_t* layer, const llmc_kv_batch_t* batch,
+                                        const llmc_attn_desc_t* attn);
+
 /* ---- measurement aid ------------------------------------------------------------- */
 
 /*

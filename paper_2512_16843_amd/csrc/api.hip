@@ -432,6 +432,157 @@ llmc_status_t llmc_materialize(const llmc_bank_t* bank, const int32_t* d_ref, in
   return launch_materialize(bank, d_ref, nullptr, nullptr, B, d_h, (hipStream_t)stream);
 }
 
+// ---- the paged key/value cache
+static llmc_status_t check_kv(const llmc_kv_desc_t* kv, bool sizes_only) {
+  REQUIRE(kv, LLMC_ERR_INVALID_ARG, "cache descriptor is NULL");
+  REQUIRE(dtype_ok(kv->dtype), LLMC_ERR_DTYPE, "cache dtype %d unknown", kv->dtype);
+  REQUIRE(kv->n_pages > 0 && kv->n_kv_heads > 0, LLMC_ERR_INVALID_ARG, "non-positive cache size");
+  REQUIRE(kv->page_size >= 16 && kv->page_size <= 1024 && (kv->page_size & (kv->page_size - 1)) == 0, LLMC_ERR_SHAPE,
+          "page_size=%d must be a power of two from 16 to 1024", kv->page_size);
+  REQUIRE(kv->head_dim == 64 || kv->head_dim == 128, LLMC_ERR_SHAPE, "head_dim must be 64 or 128, got %d", kv->head_dim);
+  REQUIRE(kv->n_kv_heads <= 65535, LLMC_ERR_SHAPE, "n_kv_heads=%d is too large", kv->n_kv_heads);
+  if (sizes_only) return LLMC_OK;
+  REQUIRE(kv->d_k && kv->d_v, LLMC_ERR_INVALID_ARG, "a cache pointer is NULL");
+  REQUIRE(aligned16(kv->d_k) && aligned16(kv->d_v), LLMC_ERR_SHAPE, "cache pointers must be 16-byte aligned");
+  return LLMC_OK;
+}
+
+// rows: whether the call takes rows of new tokens
+static llmc_status_t check_kv_batch(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, bool rows, bool sizes_only) {
+  REQUIRE(bt, LLMC_ERR_INVALID_ARG, "batch descriptor is NULL");
+  REQUIRE(bt->n_seqs > 0 && bt->max_len > 0, LLMC_ERR_INVALID_ARG, "n_seqs and max_len must be positive");
+  REQUIRE(bt->n_seqs <= LLMC_MAX_KV_SEQS, LLMC_ERR_SHAPE, "n_seqs=%d, at most %d", bt->n_seqs, LLMC_MAX_KV_SEQS);
+  REQUIRE(bt->max_len <= (1 << 30), LLMC_ERR_SHAPE, "max_len=%d, at most 2^30", bt->max_len);
+  if (rows) {
+    REQUIRE(bt->n_rows >= 0 && bt->max_new > 0, LLMC_ERR_INVALID_ARG, "n_rows must not be negative, max_new must be positive");
+    REQUIRE(bt->max_new <= bt->max_len, LLMC_ERR_SHAPE, "max_new=%d exceeds max_len=%d", bt->max_new, bt->max_len);
+  }
+  if (sizes_only) return LLMC_OK;
+  REQUIRE(bt->max_pages > 0 && (int64_t)bt->max_pages * kv->page_size >= bt->max_len, LLMC_ERR_SHAPE,
+          "max_len=%d does not fit %d pages of %d", bt->max_len, bt->max_pages, kv->page_size);
+  REQUIRE((int64_t)bt->max_pages * kv->page_size <= (1ll << 30), LLMC_ERR_SHAPE, "more than 2^30 slots a sequence");
+  REQUIRE(bt->d_table && bt->d_length, LLMC_ERR_INVALID_ARG, "page table or lengths are NULL");
+  if (rows)
+    REQUIRE(bt->d_new_start || (bt->n_rows == bt->n_seqs && bt->max_new == 1), LLMC_ERR_SHAPE,
+            "without d_new_start there is one row a sequence: n_rows = n_seqs and max_new = 1");
+  return LLMC_OK;
+}
+
+static llmc_status_t check_attn(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at) {
+  REQUIRE(at, LLMC_ERR_INVALID_ARG, "attention descriptor is NULL");
+  REQUIRE(at->n_heads > 0, LLMC_ERR_INVALID_ARG, "n_heads must be positive");
+  REQUIRE(at->n_heads % kv->n_kv_heads == 0, LLMC_ERR_SHAPE, "n_heads=%d is no multiple of n_kv_heads=%d", at->n_heads,
+          kv->n_kv_heads);
+  REQUIRE(at->n_heads <= 65535 && (int64_t)bt->max_new * at->n_heads <= 0x7FFFFFFF, LLMC_ERR_SHAPE, "n_heads=%d is too large",
+          at->n_heads);
+  REQUIRE(at->accumulate == 0 || at->accumulate == 1, LLMC_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  REQUIRE(attention_paged_grid_ok(kv->dtype, kv->n_kv_heads, at->n_heads, bt->n_rows, bt->n_seqs, bt->max_new, bt->max_len,
+                                  at->accumulate == 1), LLMC_ERR_SHAPE, "the batch is too large for one launch");
+  return LLMC_OK;
+}
+static llmc_status_t check_attn_values(const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at) {
+  REQUIRE(at->scale > 0.f && isfinite(at->scale), LLMC_ERR_INVALID_ARG, "scale must be positive and finite");
+  REQUIRE(at->softcap >= 0.f && isfinite(at->softcap), LLMC_ERR_INVALID_ARG, "softcap must be finite and not negative");
+  REQUIRE(at->window >= 0, LLMC_ERR_INVALID_ARG, "window must not be negative");
+  REQUIRE(!at->accumulate || bt->d_weight, LLMC_ERR_INVALID_ARG, "accumulate needs d_weight");
+  return LLMC_OK;
+}
+
+llmc_status_t llmc_kv_append(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const void* d_k_new, int64_t ld_k,
+                             const void* d_v_new, int64_t ld_v, const int32_t* d_pos_new, llmc_stream_t stream) {
+  LLMC_TRY(check_kv(kv, false));
+  LLMC_TRY(check_kv_batch(kv, batch, true, false));
+  REQUIRE((d_k_new && d_v_new) || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "new keys or values are NULL");
+  const int64_t row = (int64_t)kv->n_kv_heads * kv->head_dim, per = 16 / (int64_t)elem_size(kv->dtype);
+  REQUIRE(ld_k >= row && ld_v >= row && ld_k % per == 0 && ld_v % per == 0, LLMC_ERR_SHAPE,
+          "row strides must be at least n_kv_heads * head_dim and multiples of 16 bytes");
+  REQUIRE(aligned16(d_k_new) && aligned16(d_v_new), LLMC_ERR_SHAPE, "new keys and values must be 16-byte aligned");
+  return launch_kv_append(kv, batch, d_k_new, ld_k, d_v_new, ld_v, d_pos_new, (hipStream_t)stream);
+}
+
+size_t llmc_attention_paged_workspace_bytes(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch,
+                                            const llmc_attn_desc_t* attn) {
+  if (check_kv(kv, true) != LLMC_OK || check_kv_batch(kv, batch, true, true) != LLMC_OK || check_attn(kv, batch, attn) != LLMC_OK)
+    return 0;
+  return attention_paged_ws_bytes(kv->dtype, kv->head_dim, kv->n_kv_heads, attn->n_heads, batch->n_rows, batch->n_seqs,
+                                  batch->max_new, batch->max_len, attn->accumulate == 1);
+}
+
+llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const llmc_attn_desc_t* attn,
+                                   const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* d_workspace,
+                                   size_t workspace_bytes, llmc_stream_t stream) {
+  LLMC_TRY(check_kv(kv, false));
+  LLMC_TRY(check_kv_batch(kv, batch, true, false));
+  LLMC_TRY(check_attn(kv, batch, attn));
+  LLMC_TRY(check_attn_values(batch, attn));
+  REQUIRE((d_q && d_out) || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "queries or outputs are NULL");
+  const int64_t row = (int64_t)attn->n_heads * kv->head_dim, per = 16 / (int64_t)elem_size(kv->dtype);
+  REQUIRE(ld_q >= row && ld_out >= row && ld_q % per == 0 && ld_out % per == 0, LLMC_ERR_SHAPE,
+          "row strides must be at least n_heads * head_dim and multiples of 16 bytes");
+  REQUIRE(aligned16(d_q) && aligned16(d_out) && aligned16(d_workspace), LLMC_ERR_SHAPE,
+          "queries, outputs and workspace must be 16-byte aligned");
+  const size_t need = attention_paged_ws_bytes(kv->dtype, kv->head_dim, kv->n_kv_heads, attn->n_heads, batch->n_rows,
+                                               batch->n_seqs, batch->max_new, batch->max_len, attn->accumulate == 1);
+  REQUIRE(d_workspace && workspace_bytes >= need, LLMC_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  return launch_attention_paged(kv, batch, attn, d_q, ld_q, d_out, ld_out, d_workspace, (hipStream_t)stream);
+}
+
+size_t llmc_kv_evict_workspace_bytes(int32_t n_seqs, int32_t max_len) {
+  if (n_seqs <= 0 || n_seqs > LLMC_MAX_KV_SEQS || max_len <= 0 || max_len > (1 << 30)) return 0;
+  return kv_evict_ws_bytes(n_seqs, max_len);
+}
+
+llmc_status_t llmc_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const int32_t* d_keep, int32_t n_sink,
+                            int32_t n_recent, int32_t* d_length_out, void* d_workspace, size_t workspace_bytes,
+                            llmc_stream_t stream) {
+  LLMC_TRY(check_kv(kv, false));
+  LLMC_TRY(check_kv_batch(kv, batch, false, false));
+  REQUIRE(d_keep && d_length_out && batch->d_pos && batch->d_weight, LLMC_ERR_INVALID_ARG,
+          "budgets, new lengths, positions or weights are NULL");
+  REQUIRE(n_sink >= 0 && n_recent >= 0, LLMC_ERR_INVALID_ARG, "n_sink and n_recent must not be negative");
+  REQUIRE(aligned16(d_workspace), LLMC_ERR_SHAPE, "the workspace must be 16-byte aligned");
+  const size_t need = kv_evict_ws_bytes(batch->n_seqs, batch->max_len);
+  REQUIRE(d_workspace && workspace_bytes >= need, LLMC_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  return launch_kv_evict(kv, batch, d_keep, n_sink, n_recent, d_length_out, d_workspace, (hipStream_t)stream);
+}
+
+// the block's cache as far as its sizes go
+static llmc_kv_desc_t layer_kv_sizes(const llmc_layer_desc_t* L) {
+  llmc_kv_desc_t kv{};
+  kv.n_pages = 1; kv.page_size = 16; kv.n_kv_heads = L->n_heads; kv.head_dim = 64; kv.dtype = L->dtype;
+  return kv;
+}
+
+size_t llmc_layer_paged_workspace_bytes(const llmc_layer_desc_t* layer, const llmc_kv_batch_t* batch,
+                                        const llmc_attn_desc_t* attn) {
+  if (check_layer(layer) != LLMC_OK) return 0;
+  const llmc_kv_desc_t kv = layer_kv_sizes(layer);
+  if (check_kv_batch(&kv, batch, true, true) != LLMC_OK || check_attn(&kv, batch, attn) != LLMC_OK) return 0;
+  return layer_paged_ws_bytes(layer, batch->n_rows, batch->n_seqs, batch->max_new, batch->max_len, attn->accumulate == 1);
+}
+
+llmc_status_t llmc_layer_forward_paged(const llmc_layer_desc_t* layer, const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch,
+                                       const llmc_attn_desc_t* attn, const int32_t* d_pos_new, const void* d_h_in,
+                                       void* d_h_out, void* d_workspace, size_t workspace_bytes, llmc_stream_t stream) {
+  LLMC_TRY(check_layer(layer));
+  REQUIRE(layer->arch == 1, LLMC_ERR_INVALID_ARG, "only a causal decoder block (arch 1) has a key/value cache");
+  LLMC_TRY(check_kv(kv, false));
+  LLMC_TRY(check_kv_batch(kv, batch, true, false));
+  LLMC_TRY(check_attn(kv, batch, attn));
+  LLMC_TRY(check_attn_values(batch, attn));
+  REQUIRE(kv->dtype == layer->dtype, LLMC_ERR_DTYPE, "the cache and the layer have different element types");
+  REQUIRE(kv->n_kv_heads == layer->n_heads && attn->n_heads == layer->n_heads && kv->head_dim == 64, LLMC_ERR_SHAPE,
+          "the cache's heads do not fit the layer's");
+  REQUIRE((d_h_in && d_h_out) || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "d_h_in/d_h_out is NULL");
+  REQUIRE(d_h_in != d_h_out || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "d_h_in and d_h_out must not overlap");
+  REQUIRE(aligned16(d_h_in) && aligned16(d_h_out), LLMC_ERR_SHAPE, "d_h_in and d_h_out must be 16-byte aligned");
+  REQUIRE(((uintptr_t)d_workspace & 255) == 0, LLMC_ERR_SHAPE, "the workspace must be 256-byte aligned");
+  const size_t need = layer_paged_ws_bytes(layer, batch->n_rows, batch->n_seqs, batch->max_new, batch->max_len,
+                                           attn->accumulate == 1);
+  REQUIRE(d_workspace && workspace_bytes >= need, LLMC_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  return launch_layer_paged(layer, kv, batch, attn, d_pos_new, d_h_in, d_h_out, d_workspace, (hipStream_t)stream);
+}
+
 llmc_status_t llmc_profile_begin(int32_t max_records) {
   REQUIRE(max_records > 0 && max_records <= (1 << 20), LLMC_ERR_INVALID_ARG, "max_records out of range");
   REQUIRE(!g_prof_on.load() && g_prof.empty(), LLMC_ERR_INVALID_ARG, "profiling already on");

@@ -373,6 +373,25 @@ llmc_status_t launch_attention_f32(const void* qkv, void* ctx, int S, int d, int
 size_t prefix_attention_ws_bytes(const llmc_layer_desc_t* L, int B, int n_prefix);
 llmc_status_t launch_prefix_attention_mean(const llmc_layer_desc_t* L, const void* d_h, int B, int S, int n_prefix,
                                            void* ws, float* d_out, int ld_out, hipStream_t st);
+// paged.hip, paged_attn.hip: the paged key/value cache
+struct PagedArgs;
+PagedArgs paged_args(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt);
+llmc_status_t launch_kv_append(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const void* k_new, int64_t ld_k,
+                               const void* v_new, int64_t ld_v, const int32_t* pos_new, hipStream_t st);
+size_t kv_evict_ws_bytes(int n_seqs, int max_len);
+llmc_status_t launch_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const int32_t* keep, int sink, int recent,
+                              int32_t* length_out, void* ws, hipStream_t st);
+size_t attention_paged_ws_bytes(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len,
+                                bool weights);
+// whether the launches' sizes fit a grid
+bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights);
+llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at,
+                                     const void* q, int64_t ld_q, void* out, int64_t ld_out, void* ws, hipStream_t st);
+// the decoder block on new tokens (bt->n_rows of them)
+size_t layer_paged_ws_bytes(const llmc_layer_desc_t* L, int n_rows, int n_seqs, int max_new, int max_len, bool weights);
+llmc_status_t launch_layer_paged(const llmc_layer_desc_t* L, const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt,
+                                 const llmc_attn_desc_t* at, const int32_t* pos_new, const void* d_h_in, void* d_h_out,
+                                 void* ws, hipStream_t st);
 llmc_status_t launch_layer(const llmc_layer_desc_t* L, const void* d_h_in, void* d_h_out, int B, int S,
                            const int32_t* d_rows, const int32_t* d_count, void* ws, hipStream_t st,
                            float* pool_partial = nullptr, uint8_t* pooled_flags = nullptr);

@@ -365,6 +365,51 @@ static llmc_status_t layer_t(const llmc_layer_desc_t* L, const void* h_in, void*
   return LLMC_OK;
 }
 
+// ---- the decoder block on new tokens over a paged cache -------------------------------------------------
+// The same launches on n_rows rows, with the attention over whole sequences replaced by storing the new keys and values
+// and attending over the pages.
+size_t layer_paged_ws_bytes(const llmc_layer_desc_t* L, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
+  return layer_ws_bytes(L, 1, n_rows) + align_up(attention_paged_ws_bytes(L->dtype, 64, L->n_heads, L->n_heads, n_rows, n_seqs, max_new,
+                                                                          max_len, weights), 256);
+}
+
+template <typename T>
+static llmc_status_t layer_paged_t(const llmc_layer_desc_t* L, const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt,
+                                   const llmc_attn_desc_t* at, const int32_t* pos_new, const void* h_in, void* h_out, void* ws,
+                                   hipStream_t st) {
+  const int d = L->d, dff = L->d_ff, S = bt->n_rows;
+  const size_t Tn = (size_t)S, e = sizeof(T);
+  char* p = (char*)ws;
+  void* qkv = p; p += align_up(Tn * 3 * d * e, 256);
+  void* ctx = p; p += align_up(Tn * d * e, 256);
+  void* t0 = p;  p += align_up(Tn * d * e, 256);
+  void* t1 = p;  p += align_up(Tn * d * e, 256);
+  void* ff = p;  p += align_up(Tn * dff * e, 256);
+  auto gemm = [&](const void* A, const void* W, const void* bias, int N, int K, int act, const void* resid, void* out) {
+    GemmArgs a{};
+    a.S = S; a.max_seqs = 1;
+    a.A = A; a.lda = K; a.W = W; a.bias = bias; a.N = N; a.K = K; a.act = act; a.resid = resid; a.ldr = N; a.out = out; a.ldo = N;
+    return launch_gemm(a, L->dtype, st);
+  };
+  LLMC_TRY(launch_ln<T>(h_in, nullptr, t1, nullptr, L->d_ln1_g, L->d_ln1_b, L->ln_eps, d, S, nullptr, 1, st));
+  LLMC_TRY(gemm(t1, L->d_wqkv, L->d_bqkv, 3 * d, d, 0, nullptr, qkv));
+  const T* k_new = (const T*)qkv + d;
+  LLMC_TRY(launch_kv_append(kv, bt, k_new, 3 * d, k_new + d, 3 * d, pos_new, st));
+  LLMC_TRY(launch_attention_paged(kv, bt, at, qkv, 3 * d, ctx, d, p, st));
+  LLMC_TRY(gemm(ctx, L->d_wo, L->d_bo, d, d, 0, h_in, t0));
+  LLMC_TRY(launch_ln<T>(t0, nullptr, t1, nullptr, L->d_ln2_g, L->d_ln2_b, L->ln_eps, d, S, nullptr, 1, st));
+  LLMC_TRY(gemm(t1, L->d_w1, L->d_b1, dff, d, L->gelu == 0 ? 1 : 2, nullptr, ff));
+  return gemm(ff, L->d_w2, L->d_b2, d, dff, 0, t0, h_out);
+}
+
+llmc_status_t launch_layer_paged(const llmc_layer_desc_t* L, const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt,
+                                 const llmc_attn_desc_t* at, const int32_t* pos_new, const void* d_h_in, void* d_h_out,
+                                 void* ws, hipStream_t st) {
+  if (bt->n_rows == 0) return LLMC_OK;
+  if (L->dtype == LLMC_F32) return layer_paged_t<float>(L, kv, bt, at, pos_new, d_h_in, d_h_out, ws, st);
+  return layer_paged_t<bf16_t>(L, kv, bt, at, pos_new, d_h_in, d_h_out, ws, st);
+}
+
 // ---- prefix attention statistics (Section IV-B): MHA over the first tokens of every sequence ----------------------
 // out[b][t][:] = in[b][t][:] for t < n_prefix; one workgroup per token row, 16-byte vectors
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));

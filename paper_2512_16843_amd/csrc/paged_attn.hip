@@ -1,0 +1,897 @@
+// Attention of new tokens over a paged key/value cache (one token of each sequence when decoding, a chunk of each when a
+// prompt is read), and the attention weight that every cached token receives from them.
+//
+// Row m of a (sequence, key/value head) is new token m / G under query head m % G of the head's group of G, so the heads that
+// share keys are rows of one product.  With x = <q, k> * scale, optionally capped (cap * tanh(x / cap)) and lowered with
+// distance (slope_h * (pos_q - pos_k)), a row's output is sum_j p_j v_j, p = softmax of x over the keys that it sees: those
+// not behind its own slot and, with a window, less than `window` positions away.  Softmax runs once over the keys with a
+// running maximum and sum in fp32, in base 2.
+//
+// Both products are computed transposed, so that a lane holds ONE query column: S^T = K Q^T (A = keys, B = queries) and
+// O^T += V^T P^T (A = values by head dimension, B = probabilities straight from the accumulators of S^T).  The key index of
+// the second product is a free permutation, so the values are fetched in the order in which S^T delivers the keys.
+#include <algorithm>
+#include "paged.h"
+#include "mma.h"
+
+namespace llmc {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttnArgs {
+  PagedArgs p;
+  const void* q;               // [n_rows, H, DH], rows ld_q elements apart
+  void* out;                   // [n_rows, H, DH], rows ld_out elements apart
+  const void *k, *v;
+  int64_t ld_q, ld_out;
+  int32_t H, G;
+  float scale2, softcap;       // scale * log2(e)
+  float cap_in, cap_out;       // scale * 2 log2(e) / softcap, softcap * log2(e)
+  int32_t window;              // 0: none
+  const float* slopes;
+  const int32_t* pos;          // NULL: slots are positions
+  int32_t split;               // keys of one piece of a long axis, a multiple of 128
+  int32_t n_split;             // pieces that the grid provides for
+  float* part_o;               // [n_rows * H, n_split, DH], not normalised
+  float2* part_ml;             // [n_rows * H, n_split] (maximum in base 2, sum)
+  float* lse;                  // [n_rows * H] log2 of the normaliser with the maximum in it, or NULL
+};
+
+__device__ __forceinline__ float max_over_groups(float v) {      // over the four groups of 16 lanes
+  uint32_t a, b;
+  butterfly_pair_u32<32>(__float_as_uint(v), a, b);
+  v = fmaxf(__uint_as_float(a), __uint_as_float(b));
+  butterfly_pair_u32<16>(__float_as_uint(v), a, b);
+  return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ float sum_over_groups(float v) {
+  uint32_t a, b;
+  butterfly_pair_u32<32>(__float_as_uint(v), a, b);
+  v = __uint_as_float(a) + __uint_as_float(b);
+  butterfly_pair_u32<16>(__float_as_uint(v), a, b);
+  return __uint_as_float(a) + __uint_as_float(b);
+}
+
+// the keys that rows [m0, m0 + rows) of a sequence's head can see: [lo, hi), lo a multiple of 64
+struct KeyRange { int lo, hi; };
+__device__ __forceinline__ KeyRange key_range(const AttnArgs& a, const SeqRange& s, int m0, int rows) {
+  const int t0 = s.len - s.q + m0 / a.G;                                   // slot of the first row's token
+  const int t1 = s.len - s.q + min((m0 + rows - 1) / a.G, s.q - 1);
+  KeyRange r;
+  r.hi = max(t1 + 1, 0);
+  // positions rise by one at least from slot to slot unless tokens were moved, so a slot `window` away is out of the window
+  r.lo = (a.window > 0 && !a.pos) ? (int)max((int64_t)t0 - a.window + 1, (int64_t)0) & ~63 : 0;
+  return r;
+}
+
+// Scores in base 2 from products: N of them against the keys key0 + off(i).  The branches are uniform and outside the loops.
+//   capped: c (1 - 2 / (1 + 2^(x 2 log2(e) / c))), one exponential and one reciprocal, exact at both ends
+template <int N, typename Off>
+__device__ __forceinline__ void transform(const AttnArgs& a, float (&x)[N], int key0, Off off, float slope2, int t_pos,
+                                          const int32_t* pos) {
+  if (a.softcap > 0.f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float e = __builtin_amdgcn_exp2f(x[i] * a.cap_in);
+      x[i] = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + e), a.cap_out);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= a.scale2;
+  }
+  if (a.slopes || a.window > 0) {
+    int away[N];
+    if (pos) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) away[i] = t_pos - pos[min(key0 + off(i), a.p.max_len - 1)];
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) away[i] = t_pos - key0 - off(i);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = fmaf(-slope2, (float)away[i], x[i]);
+    if (a.window > 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (away[i] >= a.window) x[i] = -INFINITY;
+    }
+  }
+}
+
+// ---- pieces of the products for the two element types, 16 query columns a wavefront -----------------------------------
+template <typename T, int DH> struct Frag;
+
+template <int DH> struct Frag<bf16_t, DH> {
+  static constexpr int KEYS = 32, SUB = 2, NV = DH / 16;       // keys a step, 16-key products, output tiles of 16 dims
+  typedef uint16_t E;
+  struct Q { bf16x8_t v[DH / 32]; };
+  struct K { bf16x8_t v[SUB][DH / 32]; };
+  struct V { uint32_t w[8][NV / 2]; };                          // keys 4 g + r and 16 + 4 g + r, NV consecutive dims
+  static __device__ __forceinline__ void load_q(Q& q, const E* row, int g) {
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) q.v[i] = *reinterpret_cast<const bf16x8_t*>(row + i * 32 + g * 8);
+  }
+  static __device__ __forceinline__ void load_k(K& k, int u, const E* tile, int c, int g) {   // tile: 16 keys of one page
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) k.v[u][i] = *reinterpret_cast<const bf16x8_t*>(tile + c * DH + i * 32 + g * 8);
+  }
+  static __device__ __forceinline__ void load_v(V& v, int u, const E* tile, int c, int g) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const E* p = tile + (4 * g + r) * DH + c * NV;
+      if constexpr (NV == 4) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        v.w[u * 4 + r][0] = x.x; v.w[u * 4 + r][1] = x.y;
+      } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        v.w[u * 4 + r][0] = x.x; v.w[u * 4 + r][1] = x.y; v.w[u * 4 + r][2] = x.z; v.w[u * 4 + r][3] = x.w;
+      }
+    }
+  }
+  static __device__ __forceinline__ void clear_v(V& v, int u, int r) {
+#pragma unroll
+    for (int i = 0; i < NV / 2; ++i) v.w[u * 4 + r][i] = 0;
+  }
+  static __device__ __forceinline__ f32x4_t qk(const K& k, int u, const Q& q) {
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v[u][i], q.v[i], s, 0, 0, 0);
+    return s;
+  }
+  static __device__ __forceinline__ void pv(const V& v, const float (&p)[SUB][4], f32x4_t (&o)[NV]) {
+    union { uint32_t u[4]; bf16x8_t v; } b;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      b.u[2 * u] = f32x2_to_bf16x2(p[u][0], p[u][1]);
+      b.u[2 * u + 1] = f32x2_to_bf16x2(p[u][2], p[u][3]);
+    }
+#pragma unroll
+    for (int t = 0; t < NV; ++t) {
+      union { uint32_t u[4]; bf16x8_t v; } x;
+      const uint32_t sel = (t & 1) ? 0x07060302u : 0x05040100u;      // the high or the low halves of two keys' words
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x.u[i] = __builtin_amdgcn_perm(v.w[2 * i + 1][t >> 1], v.w[2 * i][t >> 1], sel);
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, b.v, o[t], 0, 0, 0);
+    }
+  }
+};
+
+template <int DH> struct Frag<float, DH> {
+  static constexpr int KEYS = 16, SUB = 1, NV = DH / 16;
+  typedef float E;
+  struct Q { f32x4_t v[DH / 16]; };
+  struct K { f32x4_t v[SUB][DH / 16]; };
+  struct V { f32x4_t w[4][NV / 4]; };
+  static __device__ __forceinline__ void load_q(Q& q, const E* row, int g) {
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) q.v[i] = *reinterpret_cast<const f32x4_t*>(row + i * 16 + g * 4);
+  }
+  static __device__ __forceinline__ void load_k(K& k, int u, const E* tile, int c, int g) {
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) k.v[u][i] = *reinterpret_cast<const f32x4_t*>(tile + c * DH + i * 16 + g * 4);
+  }
+  static __device__ __forceinline__ void load_v(V& v, int, const E* tile, int c, int g) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int i = 0; i < NV / 4; ++i)
+        v.w[r][i] = *reinterpret_cast<const f32x4_t*>(tile + (4 * g + r) * DH + c * NV + i * 4);
+  }
+  static __device__ __forceinline__ void clear_v(V& v, int, int r) {
+#pragma unroll
+    for (int i = 0; i < NV / 4; ++i) v.w[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  static __device__ __forceinline__ f32x4_t qk(const K& k, int u, const Q& q) {
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k.v[u][i][j], q.v[i][j], s, 0, 0, 0);
+    return s;
+  }
+  static __device__ __forceinline__ void pv(const V& v, const float (&p)[SUB][4], f32x4_t (&o)[NV]) {
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w[r][t >> 2][t & 3], p[0][r], o[t], 0, 0, 0);
+  }
+};
+
+template <typename T, int N> __device__ __forceinline__ void store_vec(T* p, const float* x);
+template <> __device__ __forceinline__ void store_vec<float, 4>(float* p, const float* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+template <> __device__ __forceinline__ void store_vec<float, 8>(float* p, const float* x) {
+  store_vec<float, 4>(p, x);
+  store_vec<float, 4>(p + 4, x + 4);
+}
+template <> __device__ __forceinline__ void store_vec<bf16_t, 4>(bf16_t* p, const float* x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]));
+}
+template <> __device__ __forceinline__ void store_vec<bf16_t, 8>(bf16_t* p, const float* x) { Vec16<bf16_t>::store(p, x); }
+
+// The block of rows that block `blk` of a launch over all sequences' row blocks works on (ROWS rows of one sequence's head
+// each): the sequence, and which of its blocks.  The wavefront counts blocks 64 sequences at a time.
+struct RowBlock { int b, mb; };
+template <int ROWS>
+__device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int blk) {
+  const int lane = threadIdx.x & 63;
+  if (!a.p.new_start) {
+    const int per = (a.G + ROWS - 1) / ROWS;
+    const RowBlock r = {blk / per, blk % per};
+    return r.b < a.p.n_seqs ? r : RowBlock{-1, 0};
+  }
+  int before = 0;
+  for (int i = 0; i < a.p.n_seqs; i += 64) {
+    const int b = i + lane;
+    int n = 0;
+    if (b < a.p.n_seqs) n = (seq_range(a.p, b).q * a.G + ROWS - 1) / ROWS;
+    int incl = n;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += v;
+    }
+    const uint64_t hit = __ballot(before + incl > blk);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      return RowBlock{__builtin_amdgcn_readfirstlane(i + l),
+                      __builtin_amdgcn_readfirstlane(blk - before - (__shfl(incl, l, 64) - __shfl(n, l, 64)))};
+    }
+    before += __shfl(incl, 63, 64);
+  }
+  return RowBlock{-1, 0};
+}
+
+// ---- few rows, or fp32: keys straight from memory to registers ----------------------------------------------------------
+// A wavefront owns 16 rows and walks the keys in steps of 32 (bf16) or 16 (fp32).  ROWSPLIT 0: the four wavefronts of a
+// workgroup take the same 16 rows and every fourth step, and join their maxima, sums and outputs in LDS: a single token's
+// keys are read once, by as many wavefronts as can be had.  ROWSPLIT 1: they take 64 rows and the same steps.
+template <typename T, int DH, bool FEAT, bool ROWSPLIT>
+__global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
+  typedef Frag<T, DH> F;
+  typedef typename F::E E;
+  constexpr int NV = F::NV, SUB = F::SUB, KEYS = F::KEYS, ROWS = ROWSPLIT ? 64 : 16, LDO = DH + 4;
+  constexpr int STEP = ROWSPLIT ? KEYS : 4 * KEYS;
+  __shared__ __attribute__((aligned(16))) float sO[ROWSPLIT ? 4 : 4 * 16 * LDO];
+  __shared__ float sM[4][16], sL[4][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const int piece = blockIdx.x % a.n_split, unit = blockIdx.x / a.n_split;
+  const int h = unit % a.p.n_kv;
+  const RowBlock rb = row_block<ROWS>(a, unit / a.p.n_kv);
+  if (rb.b < 0) return;
+  const SeqRange s = seq_range(a.p, rb.b);
+  const int rows = s.q * a.G;
+  if (rb.mb * ROWS >= rows) return;
+  const KeyRange kr = key_range(a, s, rb.mb * ROWS, ROWS);
+  const int n_pieces = max(1, (kr.hi - kr.lo + a.split - 1) / a.split);
+  if (piece >= n_pieces) return;
+  const int k_lo = kr.lo + piece * a.split;
+  int k_hi = min(kr.hi, k_lo + a.split);
+  const int m0 = rb.mb * ROWS + (ROWSPLIT ? wave * 16 : 0);
+  const int m = m0 + c;                                         // this lane's column
+  const bool row_there = m < rows;
+  const int mc = min(m, rows - 1), i_new = mc / a.G, head = h * a.G + mc % a.G;
+  const int row = s.first + i_new, t_slot = s.len - s.q + i_new;
+  const int t_first = s.len - s.q + m0 / a.G;                   // the first row's slot: all rows see the keys up to it
+  if (ROWSPLIT) k_hi = min(k_hi, max(0, s.len - s.q + min((m0 + 15) / a.G, s.q - 1) + 1));
+  const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)rb.b * a.p.max_pages << a.p.page_shift) : nullptr;
+  float slope = 0.f;
+  int t_pos = t_slot;
+  if (FEAT) {
+    if (a.slopes) slope = a.slopes[head] * kLog2e;
+    if (pos && t_slot >= 0) t_pos = pos[t_slot];
+  }
+  typename F::Q fq;
+  F::load_q(fq, (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
+  f32x4_t o[NV];
+#pragma unroll
+  for (int t = 0; t < NV; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+  const int page_mask = (1 << a.p.page_shift) - 1;
+
+  for (int kb = k_lo + (ROWSPLIT ? 0 : wave * KEYS); kb < k_hi; kb += STEP) {
+    typename F::K fk;
+    typename F::V fv;
+    bool no_page[SUB];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const int page = page_of(a.p, rb.b, kb + 16 * u);
+      no_page[u] = page < 0;
+      const size_t at = ((((size_t)max(page, 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
+      F::load_k(fk, u, (const E*)a.k + at, c, g);
+      F::load_v(fv, u, (const E*)a.v + at, c, g);
+    }
+    float x[SUB * 4];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const f32x4_t sc = F::qk(fk, u, fq);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[u * 4 + r] = sc[r];
+    }
+    bool edge = kb + KEYS - 1 > t_first || kb + KEYS > s.len;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) edge |= no_page[u];
+    if (FEAT) {
+      transform(a, x, kb + 4 * g, [](int i) { return 16 * (i >> 2) + (i & 3); }, slope, t_pos, pos);
+    } else {
+#pragma unroll
+      for (int i = 0; i < SUB * 4; ++i) x[i] *= a.scale2;
+    }
+    if (edge) {
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int key = kb + 16 * u + 4 * g + r;
+          if (key > t_slot || no_page[u]) x[u * 4 + r] = -INFINITY;
+          // what lies behind the sequence in its last page may be anything, and 0 * anything is not always 0
+          if (key >= s.len || no_page[u]) F::clear_v(fv, u, r);
+        }
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < SUB * 4; ++i) mx = fmaxf(mx, x[i]);
+    const float m_new = fmaxf(m_run, max_over_groups(mx));
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;        // a row that has seen no key so far
+    if (__any(m_new > m_run)) {
+      const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+      l_run *= corr;
+#pragma unroll
+      for (int t = 0; t < NV; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[t][r] *= corr;
+    }
+    m_run = m_new;
+    float pr[SUB][4];
+#pragma unroll
+    for (int i = 0; i < SUB * 4; ++i) {
+      pr[i >> 2][i & 3] = __builtin_amdgcn_exp2f(x[i] - m_use);
+      l_run += pr[i >> 2][i & 3];
+    }
+    F::pv(fv, pr, o);
+  }
+  l_run = sum_over_groups(l_run);
+
+  // lane: column c, dims (4 g + r) * NV + t
+  if (ROWSPLIT) {
+    if (!row_there) return;
+    const size_t rh = (size_t)row * a.H + head;
+    if (n_pieces == 1) {
+      const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float y[NV];
+#pragma unroll
+        for (int t = 0; t < NV; ++t) y[t] = o[t][r] * inv;
+        store_vec<T, NV>((T*)a.out + (size_t)row * a.ld_out + head * DH + (4 * g + r) * NV, y);
+      }
+      if (a.lse && g == 0) a.lse[rh] = l_run == 0.f ? INFINITY : m_run + __builtin_amdgcn_logf(l_run);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float y[NV];
+#pragma unroll
+        for (int t = 0; t < NV; ++t) y[t] = o[t][r];
+        store_vec<float, NV>(a.part_o + (rh * a.n_split + piece) * DH + (4 * g + r) * NV, y);
+      }
+      if (g == 0) a.part_ml[rh * a.n_split + piece] = make_float2(m_run, l_run);
+    }
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    float y[NV];
+#pragma unroll
+    for (int t = 0; t < NV; ++t) y[t] = o[t][r];
+    store_vec<float, NV>(&sO[(wave * 16 + c) * LDO + (4 * g + r) * NV], y);
+  }
+  if (g == 0) { sM[wave][c] = m_run; sL[wave][c] = l_run; }
+  __syncthreads();
+  // joined by 16 threads a row, NV dims each
+  const int jr = threadIdx.x >> 4, jd = (threadIdx.x & 15) * NV, jm = rb.mb * ROWS + jr;
+  if (jm >= rows) return;
+  float top = sM[0][jr];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) top = fmaxf(top, sM[w][jr]);
+  const float top_use = top == -INFINITY ? 0.f : top;
+  float l = 0.f, y[NV];
+#pragma unroll
+  for (int t = 0; t < NV; ++t) y[t] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sM[w][jr] - top_use);
+    l += f * sL[w][jr];
+#pragma unroll
+    for (int t = 0; t < NV; ++t) y[t] += f * sO[(w * 16 + jr) * LDO + jd + t];
+  }
+  const int jrow = s.first + jm / a.G, jhead = h * a.G + jm % a.G;
+  const size_t rh = (size_t)jrow * a.H + jhead;
+  if (n_pieces == 1) {
+    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+    for (int t = 0; t < NV; ++t) y[t] *= inv;
+    store_vec<T, NV>((T*)a.out + (size_t)jrow * a.ld_out + jhead * DH + jd, y);
+    if (a.lse && jd == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
+  } else {
+    store_vec<float, NV>(a.part_o + (rh * a.n_split + piece) * DH + jd, y);
+    if (jd == 0) a.part_ml[rh * a.n_split + piece] = make_float2(top, l);
+  }
+}
+
+// ---- the pieces of a long axis joined: a wavefront a (row, head) -------------------------------------------------------
+template <typename T, int DH, int ROWS>
+__global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
+  const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (rh >= (int64_t)a.p.n_rows * a.H) return;
+  const int lane = threadIdx.x & 63, row = (int)(rh / a.H), head = (int)(rh % a.H);
+  const int b = seq_of_row(a.p, row);
+  if (b < 0) return;
+  const SeqRange s = seq_range(a.p, b);
+  const int i = row - s.first;
+  if (i >= s.q) return;
+  const int m = i * a.G + head % a.G;
+  const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
+  const int n = max(1, (kr.hi - kr.lo + a.split - 1) / a.split);
+  if (n == 1) return;                                            // written where it was computed
+  const float2* ml = a.part_ml + rh * a.n_split;
+  const float* po = a.part_o + rh * a.n_split * DH;
+  float top = -INFINITY;
+  for (int j = lane; j < n; j += 64) top = fmaxf(top, ml[j].x);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float top_use = top == -INFINITY ? 0.f : top;
+  constexpr int PER = DH / 64;
+  float l = 0.f, y[PER];
+#pragma unroll
+  for (int t = 0; t < PER; ++t) y[t] = 0.f;
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) {
+    const float2 v = ml[j];
+    const float f = __builtin_amdgcn_exp2f(v.x - top_use);
+    l += f * v.y;
+#pragma unroll
+    for (int t = 0; t < PER; ++t) y[t] += f * po[(size_t)j * DH + t * 64 + lane];
+  }
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+  for (int t = 0; t < PER; ++t)
+    Elem<T>::store((T*)a.out + (size_t)row * a.ld_out + head * DH + t * 64 + lane, y[t] * inv);
+  if (a.lse && lane == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
+}
+
+// ---- many rows in bf16: 128 rows a workgroup share key tiles in LDS -----------------------------------------------------
+// Four wavefronts of 32 rows, key tiles of 64 (double buffered); V is transposed on its way into LDS two keys at a time, its
+// groups of four keys XOR-swizzled by the block of 32 dims so that the stores of a wavefront fall into 64 banks.
+template <int DH>
+struct TileCfg {
+  static constexpr int KT = 64, ROWS = 128;
+  static constexpr int K_STRIDE = DH + 8, V_STRIDE = KT + 4;
+  static constexpr int K_ELEMS = KT * K_STRIDE, V_ELEMS = DH * V_STRIDE;
+  static constexpr int CH = DH / 8, TR = 256 / CH;               // 16-byte chunks of a row, rows a pass of the workgroup
+  static constexpr int NK = KT / TR, NVP = KT / 2 / TR;          // K rows, V key pairs of a thread
+  static constexpr int SWZ = DH == 64 ? 4 : 2;                   // groups of four keys
+  static constexpr size_t LDS_BYTES = 2ull * (K_ELEMS + V_ELEMS) * 2;
+};
+
+template <int DH, bool FEAT>
+__global__ __launch_bounds__(256) void attention_paged_tile_kernel(AttnArgs a) {
+  typedef TileCfg<DH> C;
+  constexpr int NF = DH / 32, KS = DH / 16;
+  extern __shared__ __attribute__((aligned(16))) uint16_t tile_lds[];
+  auto sK = [&](int buf) { return tile_lds + buf * C::K_ELEMS; };
+  auto sV = [&](int buf) { return tile_lds + 2 * C::K_ELEMS + buf * C::V_ELEMS; };
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+  const int piece = blockIdx.x % a.n_split, unit = blockIdx.x / a.n_split;
+  const int h = unit % a.p.n_kv, n_blk = gridDim.x / (a.n_split * a.p.n_kv);
+  const RowBlock rb = row_block<C::ROWS>(a, n_blk - 1 - unit / a.p.n_kv);        // the last, longest blocks first
+  if (rb.b < 0) return;
+  const SeqRange s = seq_range(a.p, rb.b);
+  const int rows = s.q * a.G;
+  if (rb.mb * C::ROWS >= rows) return;
+  const KeyRange kr = key_range(a, s, rb.mb * C::ROWS, C::ROWS);
+  const int n_pieces = max(1, (kr.hi - kr.lo + a.split - 1) / a.split);
+  if (piece >= n_pieces) return;
+  const int k_lo = kr.lo + piece * a.split, k_hi = min(kr.hi, k_lo + a.split);
+  const int n_tiles = (k_hi - k_lo + C::KT - 1) / C::KT;
+  const int m0 = rb.mb * C::ROWS + wave * 32, m = m0 + (lane & 31);
+  const bool row_there = m < rows;
+  const int mc = min(m, rows - 1), i_new = mc / a.G, head = h * a.G + mc % a.G;
+  const int row = s.first + i_new, t_slot = s.len - s.q + i_new;
+  const int t_first = s.len - s.q + m0 / a.G;
+  const int t_last = s.len - s.q + min((m0 + 31) / a.G, s.q - 1);
+  const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)rb.b * a.p.max_pages << a.p.page_shift) : nullptr;
+  float slope = 0.f;
+  int t_pos = t_slot;
+  if (FEAT) {
+    if (a.slopes) slope = a.slopes[head] * kLog2e;
+    if (pos && t_slot >= 0) t_pos = pos[t_slot];
+  }
+  const uint16_t* qp = (const uint16_t*)a.q + (size_t)row * a.ld_q + head * DH;
+  bf16x8_t fq[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) fq[ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16 + half * 8);
+  f32x16_t o[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[f][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  const int st_row = tid / C::CH, st_chunk = tid % C::CH;
+  const int page_mask = (1 << a.p.page_shift) - 1;
+  uint4 rk[C::NK], rv[C::NVP][2];
+  // the 16 bytes of this thread in a key's row; zeros where there is no such key
+  auto fetch = [&](const void* base, int key) -> uint4 {
+    const int page = key < s.len ? page_of(a.p, rb.b, key) : -1;
+    if (page < 0) return make_uint4(0, 0, 0, 0);
+    return *reinterpret_cast<const uint4*>((const uint16_t*)base +
+        ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & page_mask)) * DH + st_chunk * 8);
+  };
+  auto load = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < C::NK; ++i) rk[i] = fetch(a.k, kb + st_row + i * C::TR);
+#pragma unroll
+    for (int i = 0; i < C::NVP; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) rv[i][e] = fetch(a.v, kb + 2 * (st_row + i * C::TR) + e);
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < C::NK; ++i)
+      *reinterpret_cast<uint4*>(sK(buf) + (st_row + i * C::TR) * C::K_STRIDE + st_chunk * 8) = rk[i];
+#pragma unroll
+    for (int i = 0; i < C::NVP; ++i) {
+      const int pair = st_row + i * C::TR;
+      const int key = (((pair >> 1) ^ ((st_chunk >> 2) * C::SWZ)) << 2) | ((pair & 1) << 1);
+      uint16_t* d = sV(buf) + st_chunk * 8 * C::V_STRIDE + key;
+      const uint32_t x[4] = {rv[i][0].x, rv[i][0].y, rv[i][0].z, rv[i][0].w};
+      const uint32_t y[4] = {rv[i][1].x, rv[i][1].y, rv[i][1].z, rv[i][1].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        *reinterpret_cast<uint32_t*>(d + (2 * e) * C::V_STRIDE) = (x[e] & 0xFFFFu) | (y[e] << 16);
+        *reinterpret_cast<uint32_t*>(d + (2 * e + 1) * C::V_STRIDE) = (x[e] >> 16) | (y[e] & 0xFFFF0000u);
+      }
+    }
+  };
+  if (n_tiles > 0) {
+    load(k_lo);
+    store(0);
+  }
+  __syncthreads();
+  for (int t = 0; t < n_tiles; ++t) {
+    const int buf = t & 1, kb = k_lo + t * C::KT;
+    if (t + 1 < n_tiles) load(kb + C::KT);
+    if (kb <= t_last && m0 < rows) {                             // else nothing that this wavefront's rows see
+      f32x16_t sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[u][r] = 0.f;
+      const uint16_t* kf = sK(buf) + (lane & 31) * C::K_STRIDE + half * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              *reinterpret_cast<const bf16x8_t*>(kf + u * 32 * C::K_STRIDE + ks * 16), fq[ks], sc[u], 0, 0, 0);
+      float x[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = sc[i >> 4][i & 15];
+      const auto off = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
+      const int key0 = kb + half * 4;
+      if (FEAT) {
+        transform(a, x, key0, off, slope, t_pos, pos);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] *= a.scale2;
+      }
+      if (kb + C::KT - 1 > t_first) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (key0 + off(i) > t_slot) x[i] = -INFINITY;
+      }
+      float mx = x[0];
+#pragma unroll
+      for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
+      uint32_t ma, mb_;
+      butterfly_pair_u32<32>(__float_as_uint(mx), ma, mb_);
+      mx = fmaxf(__uint_as_float(ma), __uint_as_float(mb_));
+      const float m_new = fmaxf(m_run, mx);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      if (__any(m_new > m_run)) {
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+        l_run *= corr;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[f][r] *= corr;
+      }
+      m_run = m_new;
+      uint32_t pk[2][8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(x[u * 16 + r] - m_use), p1 = __builtin_amdgcn_exp2f(x[u * 16 + r + 1] - m_use);
+          l_run += p0 + p1;
+          pk[u][r >> 1] = f32x2_to_bf16x2(p0, p1);
+        }
+      const uint16_t* vf = sV(buf) + (lane & 31) * C::V_STRIDE + half * 4;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        union { uint32_t u[4]; bf16x8_t v; } pb;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pb.u[e] = pk[ks >> 1][(ks & 1) * 4 + e];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          union { uint2 u[2]; bf16x8_t v; } va;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            va.u[i] = *reinterpret_cast<const uint2*>(vf + f * 32 * C::V_STRIDE + (((ks * 4 + 2 * i) ^ (f * C::SWZ)) << 2));
+          o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va.v, pb.v, o[f], 0, 0, 0);
+        }
+      }
+    }
+    if (t + 1 < n_tiles) store(buf ^ 1);
+    __syncthreads();
+  }
+  if (!row_there) return;
+  const float l = l_run + __shfl_xor(l_run, 32, 64);
+  const size_t rh = (size_t)row * a.H + head;
+  if (n_pieces == 1) {
+    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+    uint16_t* dst = (uint16_t*)a.out + (size_t)row * a.ld_out + head * DH + half * 4;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint2 w;
+        w.x = f32x2_to_bf16x2(o[f][4 * j] * inv, o[f][4 * j + 1] * inv);
+        w.y = f32x2_to_bf16x2(o[f][4 * j + 2] * inv, o[f][4 * j + 3] * inv);
+        *reinterpret_cast<uint2*>(dst + f * 32 + 8 * j) = w;
+      }
+    if (a.lse && half == 0) a.lse[rh] = l == 0.f ? INFINITY : m_run + __builtin_amdgcn_logf(l);
+  } else {
+    float* dst = a.part_o + (rh * a.n_split + piece) * DH + half * 4;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(dst + f * 32 + 8 * j) = make_float4(o[f][4 * j], o[f][4 * j + 1], o[f][4 * j + 2], o[f][4 * j + 3]);
+    if (half == 0) a.part_ml[rh * a.n_split + piece] = make_float2(m_run, l);
+  }
+}
+
+// ---- the weight that every key received ---------------------------------------------------------------------------------
+// sum over the rows of p = 2^(x - lse), the scores computed a second time with the finished normalisers.  A wavefront holds
+// 64 keys of one head in registers and walks the rows; its sums are per head (sums[b][h][key]), added up over the heads in
+// ascending order by the second kernel: no atomics, one order.
+constexpr int kWeightKeys = 256;                                 // a workgroup
+
+template <typename T, int DH, bool FEAT>
+__global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a, float* __restrict__ sums) {
+  typedef Frag<T, DH> F;
+  typedef typename F::E E;
+  constexpr int SUB = F::SUB, NK = 4 / SUB;                      // 4 sub-tiles of 16 keys
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const int n_kb = (a.p.max_len + kWeightKeys - 1) / kWeightKeys;
+  const int blk = blockIdx.x % n_kb, h = blockIdx.x / n_kb % a.p.n_kv, b = blockIdx.x / n_kb / a.p.n_kv;
+  const SeqRange s = seq_range(a.p, b);
+  const int kb = blk * kWeightKeys + wave * 64;
+  if (kb >= s.len) return;
+  const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)b * a.p.max_pages << a.p.page_shift) : nullptr;
+  const int page_mask = (1 << a.p.page_shift) - 1;
+  typename F::K fk[NK];
+  bool no_page[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int page = page_of(a.p, b, kb + 16 * u);
+    no_page[u] = page < 0;
+    const size_t at = ((((size_t)max(page, 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
+    F::load_k(fk[u / SUB], u % SUB, (const E*)a.k + at, c, g);
+  }
+  float w[4][4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w[u][r] = 0.f;
+  const int rows = s.q * a.G, t_base = s.len - s.q;
+  // rows whose tokens do not lie before the first key, and, with a window and slots as positions, not too far behind the last
+  const int m_lo = max(0, kb - t_base) * a.G;
+  int m_hi = rows;
+  if (a.window > 0 && !a.pos) m_hi = (int)min((int64_t)rows, max((int64_t)0, (int64_t)kb + 63 - t_base + a.window) * a.G);
+  for (int m0 = m_lo & ~15; m0 < m_hi; m0 += 16) {
+    const int m = m0 + c, mc = min(m, rows - 1), i_new = mc / a.G, head = h * a.G + mc % a.G;
+    const int row = s.first + i_new, t_slot = t_base + i_new;
+    typename F::Q fq;
+    F::load_q(fq, (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
+    const float lse = m < rows ? a.lse[(size_t)row * a.H + head] : INFINITY;
+    float slope = 0.f;
+    int t_pos = t_slot;
+    if (FEAT) {
+      if (a.slopes) slope = a.slopes[head] * kLog2e;
+      if (pos && t_slot >= 0) t_pos = pos[t_slot];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const f32x4_t sc = F::qk(fk[u / SUB], u % SUB, fq);
+      const int key0 = kb + 16 * u + 4 * g;
+      float x[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = sc[r];
+      if (FEAT) {
+        transform(a, x, key0, [](int i) { return i; }, slope, t_pos, pos);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] *= a.scale2;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        w[u][r] += key0 + r <= t_slot && !no_page[u] && lse < INFINITY ? __builtin_amdgcn_exp2f(x[r] - lse) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float v = w[u][r];
+      v += __uint_as_float(butterfly_u32<8>(__float_as_uint(v)));
+      v += __uint_as_float(butterfly_u32<4>(__float_as_uint(v)));
+      v += __uint_as_float(butterfly_u32<2>(__float_as_uint(v)));
+      v += __uint_as_float(butterfly_u32<1>(__float_as_uint(v)));
+      w[u][r] = v;
+    }
+  if (c == 0) {
+    float* dst = sums + ((size_t)b * a.p.n_kv + h) * a.p.max_len;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = kb + 16 * u + 4 * g + r;
+        if (key < s.len) dst[key] = w[u][r];
+      }
+  }
+}
+
+__global__ __launch_bounds__(256) void attention_paged_add_weights_kernel(PagedArgs p, const float* __restrict__ sums,
+                                                                          float* __restrict__ weight) {
+  const int b = blockIdx.y, key = blockIdx.x * 256 + threadIdx.x;
+  const SeqRange s = seq_range(p, b);
+  if (key >= s.len || s.q == 0) return;
+  const float* src = sums + (size_t)b * p.n_kv * p.max_len + key;
+  float v = 0.f;
+  for (int h = 0; h < p.n_kv; ++h) v += src[(size_t)h * p.max_len];
+  weight[((size_t)b * p.max_pages << p.page_shift) + key] += v;
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+struct Plan {
+  bool tile, rowsplit;
+  int rows;                    // of a row block
+  int64_t blocks;              // row blocks of all sequences, at most
+  int split, n_split;
+};
+
+// How a call is cut.  Up to 16 rows a head (single tokens above all): 16-row products with the keys dealt to wavefronts.  More
+// rows in bf16 share key tiles in LDS, in fp32 (bound by the matrix instructions of that type) 64 rows walk the keys together.
+// The key axis is cut where there are too few row blocks to fill the chip.
+Plan make_plan(int dtype, int n_rows, int n_seqs, int n_kv, int G, int max_new, int max_len) {
+  Plan p{};
+  const int64_t rows = (int64_t)max_new * G;
+  p.tile = rows > 16 && dtype == LLMC_BF16;
+  p.rowsplit = rows > 16 && !p.tile;
+  p.rows = p.tile ? 128 : p.rowsplit ? 64 : 16;
+  p.blocks = rows <= p.rows ? n_seqs : std::min<int64_t>((rows + p.rows - 1) / p.rows * n_seqs, (int64_t)n_rows * G / p.rows + n_seqs);
+  const int64_t target = p.tile ? 512 : 1024;                    // workgroups that the chip holds at once
+  const int64_t units = std::max<int64_t>(1, p.blocks * n_kv);
+  const int64_t want = std::max<int64_t>(1, target / units);
+  p.split = (int)std::max<int64_t>(256, align_up((size_t)((max_len + want - 1) / want), 128));
+  p.n_split = std::max(1, (int)((max_len + p.split - 1) / p.split));
+  return p;
+}
+
+struct Layout { size_t part_o, part_ml, lse, sums, total; };
+Layout ws_layout(const Plan& p, int n_rows, int H, int DH, int n_seqs, int n_kv, int max_len, bool weights) {
+  Layout l{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes, 256); return r; };
+  const size_t rh = (size_t)n_rows * H;
+  l.part_o = take(p.n_split > 1 ? rh * p.n_split * DH * 4 : 0);
+  l.part_ml = take(p.n_split > 1 ? rh * p.n_split * 8 : 0);
+  l.lse = take(weights ? rh * 4 : 0);
+  l.sums = take(weights ? (size_t)n_seqs * n_kv * max_len * 4 : 0);
+  l.total = std::max<size_t>(at, 256);
+  return l;
+}
+
+template <typename T, int DH, bool FEAT>
+llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* weight, hipStream_t st) {
+  const unsigned grid = (unsigned)(p.blocks * a.p.n_kv * p.n_split);
+  {
+    ProfScope ps_("attention_paged_kernel", st);
+    if constexpr (sizeof(T) == 2) {
+      if (p.tile) {
+        static std::atomic<bool> lds_set[64];
+        const auto kernel = attention_paged_tile_kernel<DH, FEAT>;
+        LLMC_TRY(ensure_dynamic_lds((const void*)kernel, TileCfg<DH>::LDS_BYTES, lds_set));
+        LLMC_KERNEL_GGL(kernel, dim3(grid), dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
+      } else {
+        LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), 0, st, a);
+      }
+    } else {
+      if (p.rowsplit) LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), dim3(grid), dim3(256), 0, st, a);
+      else LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), 0, st, a);
+    }
+  }
+  LLMC_LAUNCH_CHECK("attention_paged");
+  if (p.n_split > 1) {
+    ProfScope ps_("attention_paged_join_kernel", st);
+    const dim3 jg((unsigned)(((int64_t)a.p.n_rows * a.H + 3) / 4));
+    if (p.rows == 128) LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 128>), jg, dim3(256), 0, st, a);
+    else if (p.rows == 64) LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 64>), jg, dim3(256), 0, st, a);
+    else LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 16>), jg, dim3(256), 0, st, a);
+    LLMC_LAUNCH_CHECK("attention_paged_join");
+  }
+  if (weight) {
+    const int n_kb = (a.p.max_len + kWeightKeys - 1) / kWeightKeys;
+    { ProfScope ps_("attention_paged_weight_kernel", st);
+      LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), dim3((unsigned)((int64_t)n_kb * a.p.n_kv * a.p.n_seqs)),
+                      dim3(256), 0, st, a, sums); }
+    LLMC_LAUNCH_CHECK("attention_paged_weight");
+    { ProfScope ps_("attention_paged_add_weights_kernel", st);
+      LLMC_KERNEL_GGL(attention_paged_add_weights_kernel, dim3((a.p.max_len + 255) / 256, a.p.n_seqs), dim3(256), 0, st, a.p,
+                      sums, weight); }
+    LLMC_LAUNCH_CHECK("attention_paged_add_weights");
+  }
+  return LLMC_OK;
+}
+
+}  // namespace
+
+size_t attention_paged_ws_bytes(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len,
+                                bool weights) {
+  const Plan p = make_plan(dtype, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len);
+  return ws_layout(p, n_rows, H, head_dim, n_seqs, n_kv, max_len, weights).total;
+}
+
+bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
+  const Plan p = make_plan(dtype, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len);
+  const int64_t most = 0x7FFFFFFF;
+  return p.blocks * n_kv <= most / p.n_split && (int64_t)n_rows * H <= most &&
+         (!weights || (int64_t)((max_len + kWeightKeys - 1) / kWeightKeys) * n_kv <= most / n_seqs);
+}
+
+llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at,
+                                     const void* q, int64_t ld_q, void* out, int64_t ld_out, void* ws, hipStream_t st) {
+  if (bt->n_rows == 0) return LLMC_OK;
+  const Plan p = make_plan(kv->dtype, bt->n_rows, bt->n_seqs, kv->n_kv_heads, at->n_heads / kv->n_kv_heads, bt->max_new, bt->max_len);
+  const bool weights = bt->d_weight && at->accumulate;
+  const Layout l = ws_layout(p, bt->n_rows, at->n_heads, kv->head_dim, bt->n_seqs, kv->n_kv_heads, bt->max_len, weights);
+  AttnArgs a{};
+  a.p = paged_args(kv, bt);
+  a.q = q; a.out = out; a.k = kv->d_k; a.v = kv->d_v; a.ld_q = ld_q; a.ld_out = ld_out;
+  a.H = at->n_heads; a.G = at->n_heads / kv->n_kv_heads;
+  a.scale2 = at->scale * kLog2e; a.softcap = at->softcap;
+  if (at->softcap > 0.f) { a.cap_in = (float)(2.0 * 1.4426950408889634 * at->scale / at->softcap); a.cap_out = at->softcap * kLog2e; }
+  a.window = at->window; a.slopes = at->d_slopes;
+  a.pos = (at->window > 0 || at->d_slopes) ? bt->d_pos : nullptr;
+  a.split = p.split; a.n_split = p.n_split;
+  char* w = (char*)ws;
+  a.part_o = (float*)(w + l.part_o); a.part_ml = (float2*)(w + l.part_ml);
+  a.lse = weights ? (float*)(w + l.lse) : nullptr;
+  float* sums = weights ? (float*)(w + l.sums) : nullptr;
+  float* weight = weights ? bt->d_weight : nullptr;
+  const bool feat = at->softcap > 0.f || at->window > 0 || at->d_slopes;
+#define LLMC_PAGED(T_, DH_) \
+  return feat ? launch_t<T_, DH_, true>(a, p, sums, weight, st) : launch_t<T_, DH_, false>(a, p, sums, weight, st)
+  if (kv->dtype == LLMC_BF16) {
+    if (kv->head_dim == 64) LLMC_PAGED(bf16_t, 64);
+    LLMC_PAGED(bf16_t, 128);
+  }
+  if (kv->head_dim == 64) LLMC_PAGED(float, 64);
+  LLMC_PAGED(float, 128);
+#undef LLMC_PAGED
+}
+
+}  // namespace llmc

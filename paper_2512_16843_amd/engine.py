@@ -174,3 +174,99 @@ class GatedStack:
         for b in self.banks:
             if b is not None:
                 b.close()
+
+
+class PagedStack:
+    """A causal decoder stack that continues sequences: every layer keeps the keys and values of earlier tokens in pages, and
+    ``extend`` computes the new tokens only (a prompt, a chunk of one, or one token of each sequence; any mix).
+
+    Pages are handed out by the host from one free list; all layers share the page table and the lengths, each has its own
+    pools.  ``budget`` (with its protected ``sink`` first positions and ``recent`` last ones): after each ``extend`` every
+    layer keeps that many tokens of a sequence, those that have gathered the largest attention weight in that layer."""
+
+    def __init__(self, cfg: ModelConfig, weights, n_seqs: int, max_len: int, n_pages: Optional[int] = None,
+                 page_size: int = 16, device="cuda", budget: int = 0, sink: int = 4, recent: int = 32, window: int = 0):
+        if cfg.arch != 1:
+            raise ValueError("only a causal decoder has a key/value cache")
+        if budget and not 0 < budget <= max_len:
+            raise ValueError("the budget must lie between 1 and max_len")
+        self.cfg, self.device, self.n_seqs, self.page, self.max_len = cfg, device, n_seqs, page_size, max_len
+        self.budget, self.sink, self.recent, self.window = budget, sink, recent, window
+        self.layers = [llmc.layer_from_weights(cfg, w, device) for w in weights]
+        self.max_pages = (max_len + page_size - 1) // page_size
+        n_pages = n_seqs * self.max_pages if n_pages is None else n_pages
+        shape = (n_pages, cfg.n_heads, page_size, cfg.d // cfg.n_heads)
+        self.k = [torch.empty(shape, dtype=cfg.torch_dtype, device=device) for _ in self.layers]
+        self.v = [torch.empty(shape, dtype=cfg.torch_dtype, device=device) for _ in self.layers]
+        slots = (n_seqs, self.max_pages * page_size)
+        self.pos = [torch.zeros(slots, dtype=torch.int32, device=device) for _ in self.layers] if budget else None
+        self.weight = [torch.zeros(slots, dtype=torch.float32, device=device) for _ in self.layers] if budget else None
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.pages: List[List[int]] = [[] for _ in range(n_seqs)]
+        self.lengths = [0] * n_seqs           # tokens in the cache
+        self.next_pos = [0] * n_seqs          # tokens ever seen: the position of the next one
+        self.workspace = torch.empty((0,), dtype=torch.uint8, device=device)
+
+    def extend(self, h: torch.Tensor, new: List[int]) -> torch.Tensor:
+        """``h`` [sum(new), d]: the embedded new tokens, ``new[b]`` of them for sequence b, in order.  Returns their outputs.
+        Raises before anything is enqueued, and changes nothing, if a sequence or the pool would overflow."""
+        cfg, B = self.cfg, self.n_seqs
+        if len(new) != B or min(new) < 0 or h.dim() != 2 or h.shape[0] != sum(new):
+            raise ValueError("one count for each sequence, and a row of h for each new token")
+        if sum(new) == 0:
+            return h.new_empty(h.shape)
+        lens = [n + q for n, q in zip(self.lengths, new)]
+        if max(lens) > self.max_len:
+            raise ValueError("a sequence would hold %d tokens, max_len is %d" % (max(lens), self.max_len))
+        want = [(n + self.page - 1) // self.page - len(p) for n, p in zip(lens, self.pages)]
+        if sum(w for w in want if w > 0) > len(self.free):
+            raise ValueError("no pages left")
+        for p, w in zip(self.pages, want):
+            p.extend(self.free.pop() for _ in range(w))
+        starts = [0]
+        for q in new:
+            starts.append(starts[-1] + q)
+        # one copy brings the tables of the call: page table, lengths, starts, positions of the new tokens, budgets
+        host = [p[c] if c < len(p) else -1 for p in self.pages for c in range(self.max_pages)] + lens + starts
+        keep = [min(n, self.budget) for n in lens]
+        if self.budget:
+            host += [self.next_pos[b] + i for b in range(B) for i in range(new[b])] + keep
+        flat = torch.tensor(host, dtype=torch.int32).pin_memory().to(self.device, non_blocking=True)
+        sizes = [B * self.max_pages, B, B + 1] + ([starts[-1], B] if self.budget else [])
+        parts = flat.split(sizes)
+        table, length, start = parts[0].view(B, self.max_pages), parts[1], parts[2]
+        pos_new, keep_t = (parts[3], parts[4]) if self.budget else (None, None)
+        out = torch.empty_like(h)
+        bufs = [out, torch.empty_like(h)] if len(self.layers) > 1 else [out]
+        max_new, max_len = max(new), max(lens)
+        need = llmc.llmc_layer_paged_workspace_bytes(self.layers[0], h.shape[0], B, max_new, max_len, bool(self.budget))
+        if self.budget:
+            need = max(need, llmc.llmc_kv_evict_workspace_bytes(table, max_len))
+        if self.workspace.numel() < need:
+            self.workspace = torch.empty((need,), dtype=torch.uint8, device=self.device)
+        cut = self.budget and max(lens) > self.budget
+        left = torch.empty_like(length) if cut else None
+        x = h
+        for l, layer in enumerate(self.layers):
+            y = bufs[(len(self.layers) - 1 - l) & 1]
+            pos = self.pos[l] if self.budget else None
+            weight = self.weight[l] if self.budget else None
+            llmc.llmc_layer_forward_paged(layer, x, y, self.k[l], self.v[l], table, length, self.workspace, new_start=start,
+                                          max_new=max_new, max_len=max_len, pos_new=pos_new, pos=pos, weight=weight,
+                                          accumulate=bool(self.budget), window=self.window)
+            if cut:
+                llmc.llmc_kv_evict(self.k[l], self.v[l], table, length, pos, weight, keep_t, left, self.workspace,
+                                   max_len=max_len, sink=self.sink, recent=self.recent)
+            x = y
+        self.lengths = keep if self.budget else lens
+        self.next_pos = [n + q for n, q in zip(self.next_pos, new)]
+        for b, p in enumerate(self.pages):
+            while len(p) > (self.lengths[b] + self.page - 1) // self.page:
+                self.free.append(p.pop())
+        return out
+
+    def release(self, seq: int) -> None:
+        """Forgets sequence ``seq``; its pages are free for the next ``extend`` (on the same stream)."""
+        self.free.extend(self.pages[seq])
+        self.pages[seq], self.lengths[seq], self.next_pos[seq] = [], 0, 0
+

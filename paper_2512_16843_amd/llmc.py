@@ -34,6 +34,8 @@ EXPORTS = [
     "llmc_match_bits_workspace_bytes", "llmc_max_hamming", "llmc_bank_pool_values",
     "llmc_lsh_index_bytes", "llmc_lsh_build", "llmc_match_bits_lsh", "llmc_materialize", "llmc_match_noalloc",
     "llmc_fingerprint_prefix", "llmc_fingerprint_prefix_workspace_bytes",
+    "llmc_kv_append", "llmc_attention_paged", "llmc_attention_paged_workspace_bytes", "llmc_kv_evict",
+    "llmc_kv_evict_workspace_bytes", "llmc_layer_forward_paged", "llmc_layer_paged_workspace_bytes",
 ]
 MATCH_STATIC_SCRATCH_BYTES = 5 << 20
 
@@ -69,6 +71,22 @@ class GateOut(C.Structure):
                 ("d_counters", C.c_void_p), ("d_slots", C.c_void_p), ("d_pooled_out", C.c_void_p),
                 ("d_pooled_out_valid", C.c_void_p), ("d_key_out", C.c_void_p), ("d_key_inv_out", C.c_void_p),
                 ("d_ref_out", C.c_void_p), ("d_fp_used", C.c_void_p), ("d_inv_norm_used", C.c_void_p)]
+
+
+class KvDesc(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("d_k", C.c_void_p), ("d_v", C.c_void_p)]
+
+
+class KvBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("d_table", C.c_void_p), ("d_length", C.c_void_p),
+                ("d_new_start", C.c_void_p), ("n_rows", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32),
+                ("d_pos", C.c_void_p), ("d_weight", C.c_void_p)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int32),
+                ("d_slopes", C.c_void_p), ("accumulate", C.c_int32)]
 
 
 class LlmcError(RuntimeError):
@@ -124,6 +142,17 @@ def lib() -> C.CDLL:
         L.llmc_lsh_build.argtypes = [vp, vp, i32, i32, vp, sz, vp]
         L.llmc_match_bits_lsh.argtypes = [vp, i32, i32, vp, sz, vp, i32, i32, vp, vp, vp, vp, vp]
         L.llmc_max_hamming.restype = i32
+        kvp, btp, atp = C.POINTER(KvDesc), C.POINTER(KvBatch), C.POINTER(AttnDesc)
+        L.llmc_kv_append.argtypes = [kvp, btp, vp, i64, vp, i64, vp, vp]
+        L.llmc_attention_paged.argtypes = [kvp, btp, atp, vp, i64, vp, i64, vp, sz, vp]
+        L.llmc_attention_paged_workspace_bytes.argtypes = [kvp, btp, atp]
+        L.llmc_attention_paged_workspace_bytes.restype = sz
+        L.llmc_kv_evict.argtypes = [kvp, btp, vp, i32, i32, vp, vp, sz, vp]
+        L.llmc_kv_evict_workspace_bytes.argtypes = [i32, i32]
+        L.llmc_kv_evict_workspace_bytes.restype = sz
+        L.llmc_layer_forward_paged.argtypes = [C.POINTER(LayerDesc), kvp, btp, atp, vp, vp, vp, vp, sz, vp]
+        L.llmc_layer_paged_workspace_bytes.argtypes = [C.POINTER(LayerDesc), btp, atp]
+        L.llmc_layer_paged_workspace_bytes.restype = sz
         L.llmc_profile_begin.argtypes = [i32]
         L.llmc_profile_report.argtypes = [C.c_char_p, sz]
         L.llmc_profile_report.restype = i32
@@ -451,6 +480,197 @@ def llmc_layer_forward_gated(layer: Layer, bank: Optional[Bank], proj: Optional[
         C.byref(ld), bank.handle if bank is not None else None, C.byref(fpd), _ptr(h_in), _ptr(h_out), B, S, tau,
         flags, tick, _ptr(fp_given), _ptr(inv_norm_given), C.byref(go) if go is not None else None,
         _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# the paged key/value cache
+# ---------------------------------------------------------------------------
+
+class _Here:
+    """The tensor's device as the current one while a call enqueues (nothing to do where it is)."""
+
+    def __init__(self, t: torch.Tensor):
+        if not t.is_cuda:
+            _refuse(ERR_INVALID_ARG, "tensors must be on the GPU, got %s" % t.device)
+        self.device = t.device
+        self.other = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+        return self
+
+    def __exit__(self, *e):
+        if self.other is not None:
+            self.other.__exit__(*e)
+
+    def stream(self, stream: Optional[torch.cuda.Stream]) -> Optional[int]:
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        elif stream.device != self.device:
+            _refuse(ERR_INVALID_ARG, "a stream of %s for tensors on %s" % (stream.device, self.device))
+        return stream.cuda_stream or None
+
+
+def _refuse(status: int, msg: str) -> None:
+    raise LlmcError(status, msg)
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            _refuse(ERR_INVALID_ARG, "tensors of one call on %s and %s" % (first.device, t.device))
+
+
+def _int_ptr(t: Optional[torch.Tensor], shape, what: str) -> Optional[int]:
+    return _typed_ptr(t, torch.int32, shape, what)
+
+
+def _typed_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        _refuse(ERR_DTYPE, "%s must be %s, got %s" % (what, dtype, t.dtype))
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _refuse(ERR_SHAPE, "%s must be contiguous %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, heads: Optional[int], kd: KvDesc, dtype: torch.dtype, what: str):
+    """Pointer and row stride of [rows, heads, head_dim] whose heads are contiguous within a row."""
+    if t.dtype != dtype:
+        _refuse(ERR_DTYPE, "%s must be %s, got %s" % (what, dtype, t.dtype))
+    if t.dim() != 3 or t.shape[2] != kd.head_dim or (heads is not None and t.shape[1] != heads):
+        _refuse(ERR_SHAPE, "%s must be [rows, %s, %d], got %s" % (what, "heads" if heads is None else heads, kd.head_dim,
+                                                                  tuple(t.shape)))
+    st = t.stride()
+    if st[2] != 1 or (t.shape[1] > 1 and st[1] != kd.head_dim):
+        _refuse(ERR_SHAPE, "%s: the heads of a row must be contiguous" % what)
+    row = t.shape[1] * kd.head_dim
+    return t.data_ptr(), (st[0] if t.shape[0] > 1 else max(row, st[0]))
+
+
+def _kv_desc(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor]) -> KvDesc:
+    if k_pages.dim() != 4:
+        _refuse(ERR_SHAPE, "pages must be [n_pages, n_kv_heads, page_size, head_dim], got %s" % (tuple(k_pages.shape),))
+    n, h, p, d = k_pages.shape
+    if v_pages is not None:
+        _typed_ptr(v_pages, k_pages.dtype, k_pages.shape, "v_pages")
+    return KvDesc(n, p, h, d, dtype_code(k_pages.dtype), _typed_ptr(k_pages, k_pages.dtype, k_pages.shape, "k_pages"),
+                  None if v_pages is None else v_pages.data_ptr())
+
+
+def _kv_batch(kd: KvDesc, table, length, new_start, n_rows, max_new, max_len, pos, weight) -> KvBatch:
+    if table.dim() != 2:
+        _refuse(ERR_SHAPE, "the page table must be [n_seqs, max_pages], got %s" % (tuple(table.shape),))
+    B, mp = table.shape
+    slots = (B, mp * kd.page_size)
+    return KvBatch(B, mp, _int_ptr(table, table.shape, "table"), _int_ptr(length, (B,), "length"),
+                   _int_ptr(new_start, (B + 1,), "new_start"), n_rows, max_new, slots[1] if max_len is None else max_len,
+                   _int_ptr(pos, slots, "pos"), _typed_ptr(weight, torch.float32, slots, "weight"))
+
+
+def llmc_kv_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                   table: torch.Tensor, length: torch.Tensor, new_start: Optional[torch.Tensor] = None, max_new: int = 1,
+                   pos_new: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                   weight: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k_new, v_new [rows, n_kv_heads, head_dim] (rows may lie apart) go to the last slots of their sequences."""
+    _same_device(k_pages, k_new, v_new, v_pages, table, length, new_start, pos_new, pos, weight)
+    kd = _kv_desc(k_pages, v_pages)
+    n = k_new.shape[0]
+    if v_new.shape[0] != n:
+        _refuse(ERR_SHAPE, "k_new and v_new have different numbers of rows")
+    bd = _kv_batch(kd, table, length, new_start, n, max_new, None, pos, weight)
+    kp, ldk = _rows(k_new, kd.n_kv_heads, kd, k_pages.dtype, "k_new")
+    vp, ldv = _rows(v_new, kd.n_kv_heads, kd, k_pages.dtype, "v_new")
+    pn = _int_ptr(pos_new, (n,), "pos_new")
+    with _Here(k_pages) as here:
+        _check(lib().llmc_kv_append(C.byref(kd), C.byref(bd), kp, ldk, vp, ldv, pn, here.stream(stream)))
+
+
+def llmc_attention_paged_workspace_bytes(q: torch.Tensor, k_pages: torch.Tensor, table: torch.Tensor, max_new: int = 1,
+                                         max_len: Optional[int] = None, weights: bool = False) -> int:
+    """Only the shapes and the element type are read.  Raises for sizes that the call would refuse."""
+    kd = _kv_desc(k_pages, None)
+    slots = table.shape[1] * kd.page_size
+    bd = KvBatch(table.shape[0], table.shape[1], None, None, None, q.shape[0], max_new, slots if max_len is None else max_len)
+    ad = AttnDesc(q.shape[1], 1.0, 0.0, 0, None, 1 if weights else 0)
+    n = lib().llmc_attention_paged_workspace_bytes(C.byref(kd), C.byref(bd), C.byref(ad))
+    if n == 0:
+        _refuse(ERR_SHAPE, lib().llmc_last_error().decode())
+    return n
+
+
+def llmc_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor,
+                         length: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                         new_start: Optional[torch.Tensor] = None, max_new: int = 1, max_len: Optional[int] = None,
+                         pos: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                         scale: Optional[float] = None, softcap: float = 0.0, window: int = 0,
+                         slopes: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, out [rows, n_heads, head_dim] (rows may lie apart); ``weight`` given: the attention weights are added to it.
+    ``scale`` None: 1 / sqrt(head_dim)."""
+    _same_device(k_pages, q, v_pages, table, length, out, workspace, new_start, pos, weight, slopes)
+    kd = _kv_desc(k_pages, v_pages)
+    if out.shape[0] != q.shape[0]:
+        _refuse(ERR_SHAPE, "q and out have different numbers of rows")
+    bd = _kv_batch(kd, table, length, new_start, q.shape[0], max_new, max_len, pos, weight)
+    qp, ldq = _rows(q, None, kd, k_pages.dtype, "q")
+    op, ldo = _rows(out, q.shape[1], kd, k_pages.dtype, "out")
+    ad = AttnDesc(q.shape[1], kd.head_dim ** -0.5 if scale is None else scale, softcap, window,
+                  _typed_ptr(slopes, torch.float32, (q.shape[1],), "slopes"), 0 if weight is None else 1)
+    with _Here(k_pages) as here:
+        _check(lib().llmc_attention_paged(C.byref(kd), C.byref(bd), C.byref(ad), qp, ldq, op, ldo, _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), here.stream(stream)))
+
+
+def llmc_kv_evict_workspace_bytes(table: torch.Tensor, max_len: int) -> int:
+    return lib().llmc_kv_evict_workspace_bytes(table.shape[0], max_len)
+
+
+def llmc_kv_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+                  pos: torch.Tensor, weight: torch.Tensor, keep: torch.Tensor, length_out: torch.Tensor,
+                  workspace: torch.Tensor, max_len: Optional[int] = None, sink: int = 0, recent: int = 0,
+                  stream=None) -> None:
+    """Cuts every sequence to its ``keep`` tokens of largest accumulated weight."""
+    _same_device(k_pages, v_pages, table, length, pos, weight, keep, length_out, workspace)
+    kd = _kv_desc(k_pages, v_pages)
+    bd = _kv_batch(kd, table, length, None, 0, 1, max_len, pos, weight)
+    B = table.shape[0]
+    with _Here(k_pages) as here:
+        _check(lib().llmc_kv_evict(C.byref(kd), C.byref(bd), _int_ptr(keep, (B,), "keep"), sink, recent,
+                                   _int_ptr(length_out, (B,), "length_out"), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), here.stream(stream)))
+
+
+def llmc_layer_paged_workspace_bytes(layer: Layer, n_rows: int, n_seqs: int, max_new: int, max_len: int,
+                                     weights: bool = False) -> int:
+    ld = layer.desc()
+    bd = KvBatch(n_seqs, 0, None, None, None, n_rows, max_new, max_len)
+    ad = AttnDesc(layer.n_heads, 1.0, 0.0, 0, None, 1 if weights else 0)
+    return lib().llmc_layer_paged_workspace_bytes(C.byref(ld), C.byref(bd), C.byref(ad))
+
+
+def llmc_layer_forward_paged(layer: Layer, h_in: torch.Tensor, h_out: torch.Tensor, k_pages: torch.Tensor,
+                             v_pages: torch.Tensor, table: torch.Tensor, length: torch.Tensor, workspace: torch.Tensor,
+                             new_start: Optional[torch.Tensor] = None, max_new: int = 1, max_len: Optional[int] = None,
+                             pos_new: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                             weight: Optional[torch.Tensor] = None, accumulate: bool = False, softcap: float = 0.0,
+                             window: int = 0, slopes: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The decoder block on the new tokens h_in [rows, d]; their keys and values go to the cache.  ``accumulate``: the
+    attention weights are added to ``weight``."""
+    _same_device(k_pages, h_in, h_out, v_pages, table, length, workspace, new_start, pos_new, pos, weight, slopes)
+    n, d = h_in.shape
+    kd = _kv_desc(k_pages, v_pages)
+    bd = _kv_batch(kd, table, length, new_start, n, max_new, max_len, pos, weight)
+    ad = AttnDesc(layer.n_heads, kd.head_dim ** -0.5, softcap, window,
+                  _typed_ptr(slopes, torch.float32, (layer.n_heads,), "slopes"), 1 if accumulate else 0)
+    ld = layer.desc()
+    with _Here(k_pages) as here:
+        _check(lib().llmc_layer_forward_paged(C.byref(ld), C.byref(kd), C.byref(bd), C.byref(ad),
+                                              _int_ptr(pos_new, (n,), "pos_new"),
+                                              _typed_ptr(h_in, layer.dtype, (n, layer.d), "h_in"),
+                                              _typed_ptr(h_out, layer.dtype, (n, layer.d), "h_out"), _ptr(workspace),
+                                              workspace.numel() * workspace.element_size(), here.stream(stream)))
 
 
 def llmc_profile_begin(max_records: int) -> None:
