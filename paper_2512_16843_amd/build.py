@@ -13,9 +13,10 @@ SOURCES = ["api.hip", "fingerprint.hip", "match.hip", "bits.hip", "lsh.hip", "ga
            "dense_f32.hip", "attention.hip", "paged.hip", "paged_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-# the attention kernel feeds every matrix-instruction result to vector instructions at once: accumulators in VGPRs,
-# and its maxima need no NaN quieting (scores of finite inputs are finite or the -inf of a masked key)
-EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans", "-mno-amdgpu-ieee"]}
+# the attention kernels feed every matrix-instruction result to vector instructions at once: accumulators in VGPRs,
+# in attention.hip the maxima need no NaN quieting (scores of finite inputs are finite or the -inf of a masked key)
+EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans", "-mno-amdgpu-ieee"],
+               "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _hipcc() -> str:

@@ -462,6 +462,7 @@ static llmc_status_t check_kv_batch(const llmc_kv_desc_t* kv, const llmc_kv_batc
           "max_len=%d does not fit %d pages of %d", bt->max_len, bt->max_pages, kv->page_size);
   REQUIRE((int64_t)bt->max_pages * kv->page_size <= (1ll << 30), LLMC_ERR_SHAPE, "more than 2^30 slots a sequence");
   REQUIRE(bt->d_table && bt->d_length, LLMC_ERR_INVALID_ARG, "page table or lengths are NULL");
+  REQUIRE(aligned16(bt->d_pos) && aligned16(bt->d_weight), LLMC_ERR_SHAPE, "positions and weights must be 16-byte aligned");
   if (rows)
     REQUIRE(bt->d_new_start || (bt->n_rows == bt->n_seqs && bt->max_new == 1), LLMC_ERR_SHAPE,
             "without d_new_start there is one row a sequence: n_rows = n_seqs and max_new = 1");

@@ -18,6 +18,7 @@ namespace llmc {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 struct AttnArgs {
   PagedArgs p;
@@ -65,11 +66,10 @@ __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, const SeqRange&
   return r;
 }
 
-// Scores in base 2 from products: N of them against the keys key0 + off(i).  The branches are uniform and outside the loops.
+// Scores in base 2 from N products; at(i) is the position of the i-th key.  The branches are uniform and outside the loops.
 //   capped: c (1 - 2 / (1 + 2^(x 2 log2(e) / c))), one exponential and one reciprocal, exact at both ends
-template <int N, typename Off>
-__device__ __forceinline__ void transform(const AttnArgs& a, float (&x)[N], int key0, Off off, float slope2, int t_pos,
-                                          const int32_t* pos) {
+template <int N, typename At>
+__device__ __forceinline__ void transform(const AttnArgs& a, float (&x)[N], At at, float slope2, int t_pos) {
   if (a.softcap > 0.f) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -82,13 +82,8 @@ __device__ __forceinline__ void transform(const AttnArgs& a, float (&x)[N], int 
   }
   if (a.slopes || a.window > 0) {
     int away[N];
-    if (pos) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) away[i] = t_pos - pos[min(key0 + off(i), a.p.max_len - 1)];
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) away[i] = t_pos - key0 - off(i);
-    }
+    for (int i = 0; i < N; ++i) away[i] = t_pos - at(i);
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = fmaf(-slope2, (float)away[i], x[i]);
     if (a.window > 0) {
@@ -282,6 +277,7 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     if (a.slopes) slope = a.slopes[head] * kLog2e;
     if (pos && t_slot >= 0) t_pos = pos[t_slot];
   }
+  const int slots = a.p.max_pages << a.p.page_shift;
   typename F::Q fq;
   F::load_q(fq, (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
   f32x4_t o[NV];
@@ -313,7 +309,15 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
 #pragma unroll
     for (int u = 0; u < SUB; ++u) edge |= no_page[u];
     if (FEAT) {
-      transform(a, x, kb + 4 * g, [](int i) { return 16 * (i >> 2) + (i & 3); }, slope, t_pos, pos);
+      const int4* kp = reinterpret_cast<const int4*>(pos);
+      int key_pos[SUB * 4];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const int key0 = kb + 16 * u + 4 * g;
+        const int4 v = pos ? kp[min(key0, slots - 4) >> 2] : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
+        key_pos[u * 4] = v.x; key_pos[u * 4 + 1] = v.y; key_pos[u * 4 + 2] = v.z; key_pos[u * 4 + 3] = v.w;
+      }
+      transform(a, x, [&](int i) { return key_pos[i]; }, slope, t_pos);
     } else {
 #pragma unroll
       for (int i = 0; i < SUB * 4; ++i) x[i] *= a.scale2;
@@ -461,30 +465,66 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
 }
 
 // ---- many rows in bf16: 128 rows a workgroup share key tiles in LDS -----------------------------------------------------
-// Four wavefronts of 32 rows, key tiles of 64 (double buffered); V is transposed on its way into LDS two keys at a time, its
-// groups of four keys XOR-swizzled by the block of 32 dims so that the stores of a wavefront fall into 64 banks.
+// Four wavefronts of 32 rows, tiles of 64 keys and values, double buffered, filled by direct global -> LDS loads: a load
+// instruction of a wavefront fills 1 KiB, rows of one page, so its page is a scalar.  Values stay as they lie in memory and are
+// transposed by the LDS's transposing reads (a group of 16 lanes gets 4 keys of 16 dims, 4 keys a lane).  The 16-byte chunks of a row are
+// XOR-swizzled by the row, on the global side: 16 consecutive rows then offer one chunk in 16 places (the keys' 16-byte reads), and four consecutive
+// rows four neighbouring chunks in 4 different quarters of the banks (the values' transposing reads).
 template <int DH>
 struct TileCfg {
   static constexpr int KT = 64, ROWS = 128;
-  static constexpr int K_STRIDE = DH + 8, V_STRIDE = KT + 4;
-  static constexpr int K_ELEMS = KT * K_STRIDE, V_ELEMS = DH * V_STRIDE;
-  static constexpr int CH = DH / 8, TR = 256 / CH;               // 16-byte chunks of a row, rows a pass of the workgroup
-  static constexpr int NK = KT / TR, NVP = KT / 2 / TR;          // K rows, V key pairs of a thread
-  static constexpr int SWZ = DH == 64 ? 4 : 2;                   // groups of four keys
-  static constexpr size_t LDS_BYTES = 2ull * (K_ELEMS + V_ELEMS) * 2;
+  static constexpr int CH = DH / 8;                               // 16-byte chunks of a row
+  static constexpr int RPI = 64 / CH;                             // rows that one load instruction of a wavefront fills
+  static constexpr int NI = KT / RPI / 4;                         // load instructions of a wavefront, for K and for V
+  static constexpr int TILE = KT * DH;                            // elements
+  static constexpr size_t LDS_BYTES = 4ull * TILE * 2 + 2 * KT * 4;  // and the tiles' positions
+  // place of chunk c of row r: c ^ swz(r)
+  static __device__ __forceinline__ int swz(int r) {
+    if (DH == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    return (((r >> 1) & 1) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+  }
 };
 
+// 64 entries of a sequence's row of the page table in a wavefront's registers
+struct PageWindow {
+  const int32_t* row;
+  int last, n_pages, base, ids;
+  __device__ __forceinline__ PageWindow(const PagedArgs& p, int b, int col)
+      : row(p.table + (size_t)b * p.max_pages), last(p.max_pages - 1), n_pages(p.n_pages) { fill(col); }
+  __device__ __forceinline__ void fill(int col) {
+    base = col;
+    ids = row[min(col + (int)(threadIdx.x & 63), last)];
+  }
+  // before the columns first .. last (fewer than 64) are asked for: a load, and the wait for it, must not come between others
+  __device__ __forceinline__ void cover(int first, int last_col) {
+    if (last_col - base >= 64) fill(first);
+  }
+  // page of a column that all lanes ask for, -1 if it is none
+  __device__ __forceinline__ int at(int col) const {
+    const int p = __builtin_amdgcn_readlane(ids, col - base);
+    return (uint32_t)p < (uint32_t)n_pages ? p : -1;
+  }
+};
+
+typedef short v4s16_t __attribute__((ext_vector_type(4)));
+// (`restrict` gives the read alias information once inlined.  Without any, the compiler takes it to depend on every direct
+// global -> LDS load in flight and waits for the next tile here.)
+typedef __attribute__((address_space(3))) v4s16_t lds_v4s16_t;
+__device__ __forceinline__ v4s16_t lds_read_tr(lds_v4s16_t* __restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
+__device__ __forceinline__ uint2 lds_read_transposed(const uint16_t* p) {
+  return __builtin_bit_cast(uint2, lds_read_tr((lds_v4s16_t*)p));
+}
+
 template <int DH, bool FEAT>
-__global__ __launch_bounds__(256) void attention_paged_tile_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_kernel(AttnArgs a) {
   typedef TileCfg<DH> C;
   constexpr int NF = DH / 32, KS = DH / 16;
   extern __shared__ __attribute__((aligned(16))) uint16_t tile_lds[];
-  auto sK = [&](int buf) { return tile_lds + buf * C::K_ELEMS; };
-  auto sV = [&](int buf) { return tile_lds + 2 * C::K_ELEMS + buf * C::V_ELEMS; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int piece = blockIdx.x % a.n_split, unit = blockIdx.x / a.n_split;
-  const int h = unit % a.p.n_kv, n_blk = gridDim.x / (a.n_split * a.p.n_kv);
-  const RowBlock rb = row_block<C::ROWS>(a, n_blk - 1 - unit / a.p.n_kv);        // the last, longest blocks first
+  // the heads of a row block on neighbouring workgroups: with a multiple of eight heads each XCD keeps its own in its L2
+  const int h = blockIdx.x % a.p.n_kv, piece = blockIdx.x / a.p.n_kv % a.n_split;
+  const int n_blk = gridDim.x / (a.n_split * a.p.n_kv);
+  const RowBlock rb = row_block<C::ROWS>(a, n_blk - 1 - blockIdx.x / a.p.n_kv / a.n_split);     // the last, longest blocks first
   if (rb.b < 0) return;
   const SeqRange s = seq_range(a.p, rb.b);
   const int rows = s.q * a.G;
@@ -507,6 +547,34 @@ __global__ __launch_bounds__(256) void attention_paged_tile_kernel(AttnArgs a) {
     if (a.slopes) slope = a.slopes[head] * kLog2e;
     if (pos && t_slot >= 0) t_pos = pos[t_slot];
   }
+
+  PageWindow pages(a.p, rb.b, k_lo >> a.p.page_shift);
+  const int slots = a.p.max_pages << a.p.page_shift;
+  const int page_mask = (1 << a.p.page_shift) - 1;
+  // this lane's row and chunk in a load instruction; the swizzle looks at rows modulo 16, so it differs between instructions
+  const int ld_row = lane / C::CH, ld_slot = lane % C::CH;
+  bool bad_next = false;                                          // whether the tile being loaded has a page that is none
+  auto load = [&](int kb, int buf) {
+    pages.cover(kb >> a.p.page_shift, (kb + C::KT - 1) >> a.p.page_shift);
+    bad_next = false;
+    for (int col = kb >> a.p.page_shift; col <= (min(kb + C::KT, s.len) - 1) >> a.p.page_shift; ++col)
+      bad_next |= pages.at(col) < 0;
+    if (FEAT && pos && wave == 3)
+      __builtin_amdgcn_global_load_lds(LLMC_GPTR(pos + min(kb + lane, slots - 1)),
+                                       LLMC_LPTR(tile_lds + 4 * C::TILE + buf * 2 * C::KT), 4, 0, 0);
+#pragma unroll
+    for (int j = 0; j < C::NI; ++j) {
+      const int r0 = (wave * C::NI + j) * C::RPI, key = kb + r0;
+      const int page = max(pages.at(key >> a.p.page_shift), 0);
+      const size_t at = ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & page_mask)) * DH;
+      const int off = ld_row * DH + (ld_slot ^ C::swz(r0 + ld_row)) * 8;
+      uint16_t* dst = tile_lds + buf * 2 * C::TILE + r0 * DH;
+      __builtin_amdgcn_global_load_lds(LLMC_GPTR((const uint16_t*)a.k + at + off), LLMC_LPTR(dst), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(LLMC_GPTR((const uint16_t*)a.v + at + off), LLMC_LPTR(dst + C::TILE), 16, 0, 0);
+    }
+  };
+  if (n_tiles > 0) load(k_lo, 0);
+
   const uint16_t* qp = (const uint16_t*)a.q + (size_t)row * a.ld_q + head * DH;
   bf16x8_t fq[KS];
 #pragma unroll
@@ -517,124 +585,115 @@ __global__ __launch_bounds__(256) void attention_paged_tile_kernel(AttnArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[f][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
+  const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+  const bool exact_sum = a.lse != nullptr;
+  // fragment places: keys' row lane % 32 (the swizzle looks at 16 rows), values' row (lane % 16) / 4 of a group of four keys
+  const int k_row = lane & 31, k_swz = C::swz(k_row);
+  const int v_row = half * 4 + ((lane & 15) >> 2), v_col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 
-  const int st_row = tid / C::CH, st_chunk = tid % C::CH;
-  const int page_mask = (1 << a.p.page_shift) - 1;
-  uint4 rk[C::NK], rv[C::NVP][2];
-  // the 16 bytes of this thread in a key's row; zeros where there is no such key
-  auto fetch = [&](const void* base, int key) -> uint4 {
-    const int page = key < s.len ? page_of(a.p, rb.b, key) : -1;
-    if (page < 0) return make_uint4(0, 0, 0, 0);
-    return *reinterpret_cast<const uint4*>((const uint16_t*)base +
-        ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & page_mask)) * DH + st_chunk * 8);
-  };
-  auto load = [&](int kb) {
-#pragma unroll
-    for (int i = 0; i < C::NK; ++i) rk[i] = fetch(a.k, kb + st_row + i * C::TR);
-#pragma unroll
-    for (int i = 0; i < C::NVP; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) rv[i][e] = fetch(a.v, kb + 2 * (st_row + i * C::TR) + e);
-  };
-  auto store = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < C::NK; ++i)
-      *reinterpret_cast<uint4*>(sK(buf) + (st_row + i * C::TR) * C::K_STRIDE + st_chunk * 8) = rk[i];
-#pragma unroll
-    for (int i = 0; i < C::NVP; ++i) {
-      const int pair = st_row + i * C::TR;
-      const int key = (((pair >> 1) ^ ((st_chunk >> 2) * C::SWZ)) << 2) | ((pair & 1) << 1);
-      uint16_t* d = sV(buf) + st_chunk * 8 * C::V_STRIDE + key;
-      const uint32_t x[4] = {rv[i][0].x, rv[i][0].y, rv[i][0].z, rv[i][0].w};
-      const uint32_t y[4] = {rv[i][1].x, rv[i][1].y, rv[i][1].z, rv[i][1].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        *reinterpret_cast<uint32_t*>(d + (2 * e) * C::V_STRIDE) = (x[e] & 0xFFFFu) | (y[e] << 16);
-        *reinterpret_cast<uint32_t*>(d + (2 * e + 1) * C::V_STRIDE) = (x[e] >> 16) | (y[e] & 0xFFFF0000u);
-      }
-    }
-  };
-  if (n_tiles > 0) {
-    load(k_lo);
-    store(0);
-  }
-  __syncthreads();
   for (int t = 0; t < n_tiles; ++t) {
     const int buf = t & 1, kb = k_lo + t * C::KT;
-    if (t + 1 < n_tiles) load(kb + C::KT);
-    if (kb <= t_last && m0 < rows) {                             // else nothing that this wavefront's rows see
-      f32x16_t sc[2];
+    const bool bad = bad_next;
+    LLMC_WAIT_VM(0);
+    dma::barrier();                                               // this tile is there, and the other buffer's readers are done
+    if (t + 1 < n_tiles) load(kb + C::KT, buf ^ 1);
+    uint16_t* sk = tile_lds + buf * 2 * C::TILE;
+    uint16_t* sv = sk + C::TILE;
+    if (kb + C::KT > s.len || bad) {
+      // what lies behind the sequence in its last page may be anything, and 0 * anything is not always 0
+      const int r = tid >> 2, key = kb + r;
+      if (key >= s.len || page_of(a.p, rb.b, key) < 0) {
+#pragma unroll
+        for (int i = 0; i < C::CH / 4; ++i)
+          *reinterpret_cast<uint4*>(sv + r * DH + ((tid & 3) * (C::CH / 4) + i) * 8) = make_uint4(0, 0, 0, 0);
+      }
+      __syncthreads();
+    }
+    if (kb > t_last || m0 >= rows) continue;                      // nothing that this wavefront's rows see
+    f32x16_t sc[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[u][r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
+        sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            *reinterpret_cast<const bf16x8_t*>(sk + (u * 32 + k_row) * DH + (((ks * 2 + half) ^ k_swz) << 3)), fq[ks], sc[u], 0, 0, 0);
+    float x[32];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[u][r] = 0.f;
-      const uint16_t* kf = sK(buf) + (lane & 31) * C::K_STRIDE + half * 8;
+    for (int i = 0; i < 32; ++i) x[i] = sc[i >> 4][i & 15];
+    const auto off = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
+    const int key0 = kb + half * 4;
+    if (FEAT) {
+      const int* tile_pos = reinterpret_cast<const int*>(tile_lds + 4 * C::TILE + buf * 2 * C::KT) + half * 4;
+      transform(a, x, [&](int i) { return pos ? tile_pos[off(i)] : key0 + off(i); }, slope, t_pos);
+    }
+    if (kb + C::KT - 1 > t_first) {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+      for (int i = 0; i < 32; ++i)
+        if (key0 + off(i) > t_slot) x[i] = -INFINITY;
+    }
+    if (bad) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              *reinterpret_cast<const bf16x8_t*>(kf + u * 32 * C::K_STRIDE + ks * 16), fq[ks], sc[u], 0, 0, 0);
-      float x[32];
+      for (int i = 0; i < 32; ++i)
+        if (page_of(a.p, rb.b, min(key0 + off(i), a.p.max_len - 1)) < 0) x[i] = -INFINITY;
+    }
+    float mx = x[0];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = sc[i >> 4][i & 15];
-      const auto off = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
-      const int key0 = kb + half * 4;
-      if (FEAT) {
-        transform(a, x, key0, off, slope, t_pos, pos);
-      } else {
+    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
+    uint32_t ma, mb_;
+    butterfly_pair_u32<32>(__float_as_uint(mx), ma, mb_);
+    mx = fmaxf(__uint_as_float(ma), __uint_as_float(mb_));
+    const float m_new = fmaxf(m_run, FEAT ? mx : mx * a.scale2);
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    if (__any(m_new > m_run)) {
+      const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+      l_run *= corr;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] *= a.scale2;
-      }
-      if (kb + C::KT - 1 > t_first) {
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (key0 + off(i) > t_slot) x[i] = -INFINITY;
-      }
-      float mx = x[0];
+        for (int r = 0; r < 16; ++r) o[f][r] *= corr;
+    }
+    m_run = m_new;
+    // the scale (of scores that are not transformed) enters the exponent as one fma
+    uint32_t pk[2][8];
+    float l_exact = 0.f;
 #pragma unroll
-      for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
-      uint32_t ma, mb_;
-      butterfly_pair_u32<32>(__float_as_uint(mx), ma, mb_);
-      mx = fmaxf(__uint_as_float(ma), __uint_as_float(mb_));
-      const float m_new = fmaxf(m_run, mx);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      if (__any(m_new > m_run)) {
-        const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
-        l_run *= corr;
+    for (int i = 0; i < 32; i += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(FEAT ? x[i] - m_use : fmaf(x[i], a.scale2, -m_use));
+      const float p1 = __builtin_amdgcn_exp2f(FEAT ? x[i + 1] - m_use : fmaf(x[i + 1], a.scale2, -m_use));
+      pk[i >> 4][(i & 15) >> 1] = f32x2_to_bf16x2(p0, p1);
+      x[i] = p0; x[i + 1] = p1;
+    }
+    // The sum is that of the rounded weights, two an instruction: the weights of the value product then add up to one.  Where
+    // the cached tokens' weights are wanted too, which are not rounded, it is that of the weights as they are.
+    if (exact_sum) {
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
+      for (int i = 0; i < 32; ++i) l_exact += x[i];
+      l_run += l_exact;
+    } else {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[f][r] *= corr;
-      }
-      m_run = m_new;
-      uint32_t pk[2][8];
+      for (int e = 0; e < 16; ++e)
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[e >> 3][e & 7]), ones, l_run, false);
+    }
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+    for (int ks = 0; ks < 4; ++ks) {
+      union { uint32_t u[4]; bf16x8_t v; } pb;
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(x[u * 16 + r] - m_use), p1 = __builtin_amdgcn_exp2f(x[u * 16 + r + 1] - m_use);
-          l_run += p0 + p1;
-          pk[u][r >> 1] = f32x2_to_bf16x2(p0, p1);
+      for (int e = 0; e < 4; ++e) pb.u[e] = pk[ks >> 1][(ks & 1) * 4 + e];
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        union { uint2 u[2]; bf16x8_t v; } va;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = ks * 16 + i * 8 + v_row, col = f * 32 + v_col;
+          va.u[i] = lds_read_transposed(sv + r * DH + (((col >> 3) ^ C::swz(r)) << 3) + (col & 7));
         }
-      const uint16_t* vf = sV(buf) + (lane & 31) * C::V_STRIDE + half * 4;
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        union { uint32_t u[4]; bf16x8_t v; } pb;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pb.u[e] = pk[ks >> 1][(ks & 1) * 4 + e];
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-          union { uint2 u[2]; bf16x8_t v; } va;
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            va.u[i] = *reinterpret_cast<const uint2*>(vf + f * 32 * C::V_STRIDE + (((ks * 4 + 2 * i) ^ (f * C::SWZ)) << 2));
-          o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va.v, pb.v, o[f], 0, 0, 0);
-        }
+        o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va.v, pb.v, o[f], 0, 0, 0);
       }
     }
-    if (t + 1 < n_tiles) store(buf ^ 1);
-    __syncthreads();
   }
   if (!row_there) return;
   const float l = l_run + __shfl_xor(l_run, 32, 64);
@@ -680,6 +739,7 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
   const SeqRange s = seq_range(a.p, b);
   const int kb = blk * kWeightKeys + wave * 64;
   if (kb >= s.len) return;
+  const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)b * a.p.max_pages << a.p.page_shift) : nullptr;
   const int page_mask = (1 << a.p.page_shift) - 1;
   typename F::K fk[NK];
@@ -721,7 +781,10 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[r] = sc[r];
       if (FEAT) {
-        transform(a, x, key0, [](int i) { return i; }, slope, t_pos, pos);
+        const int4 v = pos ? reinterpret_cast<const int4*>(pos)[min(key0, slots - 4) >> 2]
+                           : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
+        const int key_pos[4] = {v.x, v.y, v.z, v.w};
+        transform(a, x, [&](int i) { return key_pos[i]; }, slope, t_pos);
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] *= a.scale2;

@@ -486,88 +486,81 @@ def llmc_layer_forward_gated(layer: Layer, bank: Optional[Bank], proj: Optional[
 # the paged key/value cache
 # ---------------------------------------------------------------------------
 
-class _Here:
-    """The tensor's device as the current one while a call enqueues (nothing to do where it is)."""
-
-    def __init__(self, t: torch.Tensor):
-        if not t.is_cuda:
-            _refuse(ERR_INVALID_ARG, "tensors must be on the GPU, got %s" % t.device)
-        self.device = t.device
-        self.other = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-        return self
-
-    def __exit__(self, *e):
-        if self.other is not None:
-            self.other.__exit__(*e)
-
-    def stream(self, stream: Optional[torch.cuda.Stream]) -> Optional[int]:
-        if stream is None:
-            stream = torch.cuda.current_stream()
-        elif stream.device != self.device:
-            _refuse(ERR_INVALID_ARG, "a stream of %s for tensors on %s" % (stream.device, self.device))
-        return stream.cuda_stream or None
-
+# These calls run once a layer and token, so their checks cost as little as they can: one comparison a property, and the
+# message is made only where one fails.
 
 def _refuse(status: int, msg: str) -> None:
     raise LlmcError(status, msg)
 
 
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    for t in others:
-        if t is not None and t.device != first.device:
-            _refuse(ERR_INVALID_ARG, "tensors of one call on %s and %s" % (first.device, t.device))
-
-
-def _int_ptr(t: Optional[torch.Tensor], shape, what: str) -> Optional[int]:
-    return _typed_ptr(t, torch.int32, shape, what)
-
-
-def _typed_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str) -> Optional[int]:
-    if t is None:
-        return None
-    if t.dtype != dtype:
+def _at(t: torch.Tensor, dtype: torch.dtype, shape, dev: int, what: str) -> int:
+    """Pointer of a contiguous tensor of that type and shape on that device."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype:
         _refuse(ERR_DTYPE, "%s must be %s, got %s" % (what, dtype, t.dtype))
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        _refuse(ERR_SHAPE, "%s must be contiguous %s, got %s" % (what, tuple(shape), tuple(t.shape)))
-    return t.data_ptr()
+    if t.get_device() != dev:
+        _refuse(ERR_INVALID_ARG, "%s is on %s, the pages are on device %d" % (what, t.device, dev))
+    _refuse(ERR_SHAPE, "%s must be contiguous %s, got %s" % (what, tuple(shape), tuple(t.shape)))
 
 
-def _rows(t: torch.Tensor, heads: Optional[int], kd: KvDesc, dtype: torch.dtype, what: str):
+def _rows(t: torch.Tensor, heads: int, head_dim: int, dtype: torch.dtype, dev: int, what: str):
     """Pointer and row stride of [rows, heads, head_dim] whose heads are contiguous within a row."""
-    if t.dtype != dtype:
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype:
         _refuse(ERR_DTYPE, "%s must be %s, got %s" % (what, dtype, t.dtype))
-    if t.dim() != 3 or t.shape[2] != kd.head_dim or (heads is not None and t.shape[1] != heads):
-        _refuse(ERR_SHAPE, "%s must be [rows, %s, %d], got %s" % (what, "heads" if heads is None else heads, kd.head_dim,
-                                                                  tuple(t.shape)))
-    st = t.stride()
-    if st[2] != 1 or (t.shape[1] > 1 and st[1] != kd.head_dim):
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
+        _refuse(ERR_SHAPE, "%s must be [rows, %d, %d], got %s" % (what, heads, head_dim, tuple(shape)))
+    if stride[2] != 1 or (heads > 1 and stride[1] != head_dim):
         _refuse(ERR_SHAPE, "%s: the heads of a row must be contiguous" % what)
-    row = t.shape[1] * kd.head_dim
-    return t.data_ptr(), (st[0] if t.shape[0] > 1 else max(row, st[0]))
+    if t.get_device() != dev:
+        _refuse(ERR_INVALID_ARG, "%s is on %s, the pages are on device %d" % (what, t.device, dev))
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else max(heads * head_dim, stride[0]))
 
 
-def _kv_desc(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor]) -> KvDesc:
-    if k_pages.dim() != 4:
-        _refuse(ERR_SHAPE, "pages must be [n_pages, n_kv_heads, page_size, head_dim], got %s" % (tuple(k_pages.shape),))
-    n, h, p, d = k_pages.shape
-    if v_pages is not None:
-        _typed_ptr(v_pages, k_pages.dtype, k_pages.shape, "v_pages")
-    return KvDesc(n, p, h, d, dtype_code(k_pages.dtype), _typed_ptr(k_pages, k_pages.dtype, k_pages.shape, "k_pages"),
-                  None if v_pages is None else v_pages.data_ptr())
+def _kv_desc(k_pages: torch.Tensor, v_pages: torch.Tensor, dev: int) -> KvDesc:
+    shape, dt = k_pages.shape, k_pages.dtype
+    if len(shape) != 4:
+        _refuse(ERR_SHAPE, "pages must be [n_pages, n_kv_heads, page_size, head_dim], got %s" % (tuple(shape),))
+    return KvDesc(shape[0], shape[2], shape[1], shape[3], dtype_code(dt), _at(k_pages, dt, shape, dev, "k_pages"),
+                  _at(v_pages, dt, shape, dev, "v_pages"))
 
 
-def _kv_batch(kd: KvDesc, table, length, new_start, n_rows, max_new, max_len, pos, weight) -> KvBatch:
-    if table.dim() != 2:
-        _refuse(ERR_SHAPE, "the page table must be [n_seqs, max_pages], got %s" % (tuple(table.shape),))
-    B, mp = table.shape
-    slots = (B, mp * kd.page_size)
-    return KvBatch(B, mp, _int_ptr(table, table.shape, "table"), _int_ptr(length, (B,), "length"),
-                   _int_ptr(new_start, (B + 1,), "new_start"), n_rows, max_new, slots[1] if max_len is None else max_len,
-                   _int_ptr(pos, slots, "pos"), _typed_ptr(weight, torch.float32, slots, "weight"))
+def _kv_batch(page_size: int, dev: int, table, length, new_start, n_rows, max_new, max_len, pos, weight) -> KvBatch:
+    shape = table.shape
+    if len(shape) != 2:
+        _refuse(ERR_SHAPE, "the page table must be [n_seqs, max_pages], got %s" % (tuple(shape),))
+    B, mp = shape
+    i32 = torch.int32
+    slots = mp * page_size
+    return KvBatch(B, mp, _at(table, i32, shape, dev, "table"), _at(length, i32, (B,), dev, "length"),
+                   None if new_start is None else _at(new_start, i32, (B + 1,), dev, "new_start"), n_rows, max_new,
+                   slots if max_len is None else max_len,
+                   None if pos is None else _at(pos, i32, (B, slots), dev, "pos"),
+                   None if weight is None else _at(weight, torch.float32, (B, slots), dev, "weight"))
+
+
+def _workspace(t: torch.Tensor, dev: int):
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(ERR_INVALID_ARG, "the workspace must be contiguous and on the pages' device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _enqueue(fn, dev: int, stream: Optional[torch.cuda.Stream], *args) -> None:
+    """fn(*args, stream) with the tensors' device as the current one; no stream given: that device's current one."""
+    if dev < 0:
+        _refuse(ERR_INVALID_ARG, "tensors must be on the GPU")
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(dev)       # torch.cuda.current_stream() makes an object: 2.5 us
+    else:
+        if stream.device_index != dev:
+            _refuse(ERR_INVALID_ARG, "a stream of device %d for tensors on device %d" % (stream.device_index, dev))
+        raw = stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        _check(fn(*args, raw or None))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, raw or None))
 
 
 def llmc_kv_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -575,27 +568,26 @@ def llmc_kv_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tens
                    pos_new: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
                    weight: Optional[torch.Tensor] = None, stream=None) -> None:
     """k_new, v_new [rows, n_kv_heads, head_dim] (rows may lie apart) go to the last slots of their sequences."""
-    _same_device(k_pages, k_new, v_new, v_pages, table, length, new_start, pos_new, pos, weight)
-    kd = _kv_desc(k_pages, v_pages)
-    n = k_new.shape[0]
+    dev = k_pages.get_device()
+    kd = _kv_desc(k_pages, v_pages, dev)
+    n, dt = k_new.shape[0], k_pages.dtype
     if v_new.shape[0] != n:
         _refuse(ERR_SHAPE, "k_new and v_new have different numbers of rows")
-    bd = _kv_batch(kd, table, length, new_start, n, max_new, None, pos, weight)
-    kp, ldk = _rows(k_new, kd.n_kv_heads, kd, k_pages.dtype, "k_new")
-    vp, ldv = _rows(v_new, kd.n_kv_heads, kd, k_pages.dtype, "v_new")
-    pn = _int_ptr(pos_new, (n,), "pos_new")
-    with _Here(k_pages) as here:
-        _check(lib().llmc_kv_append(C.byref(kd), C.byref(bd), kp, ldk, vp, ldv, pn, here.stream(stream)))
+    bd = _kv_batch(kd.page_size, dev, table, length, new_start, n, max_new, None, pos, weight)
+    kp, ldk = _rows(k_new, kd.n_kv_heads, kd.head_dim, dt, dev, "k_new")
+    vp, ldv = _rows(v_new, kd.n_kv_heads, kd.head_dim, dt, dev, "v_new")
+    pn = None if pos_new is None else _at(pos_new, torch.int32, (n,), dev, "pos_new")
+    _enqueue(lib().llmc_kv_append, dev, stream, kd, bd, kp, ldk, vp, ldv, pn)
 
 
 def llmc_attention_paged_workspace_bytes(q: torch.Tensor, k_pages: torch.Tensor, table: torch.Tensor, max_new: int = 1,
                                          max_len: Optional[int] = None, weights: bool = False) -> int:
     """Only the shapes and the element type are read.  Raises for sizes that the call would refuse."""
-    kd = _kv_desc(k_pages, None)
+    kd = _kv_desc(k_pages, k_pages, k_pages.get_device())
     slots = table.shape[1] * kd.page_size
     bd = KvBatch(table.shape[0], table.shape[1], None, None, None, q.shape[0], max_new, slots if max_len is None else max_len)
     ad = AttnDesc(q.shape[1], 1.0, 0.0, 0, None, 1 if weights else 0)
-    n = lib().llmc_attention_paged_workspace_bytes(C.byref(kd), C.byref(bd), C.byref(ad))
+    n = lib().llmc_attention_paged_workspace_bytes(kd, bd, ad)
     if n == 0:
         _refuse(ERR_SHAPE, lib().llmc_last_error().decode())
     return n
@@ -609,18 +601,19 @@ def llmc_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
                          slopes: Optional[torch.Tensor] = None, stream=None) -> None:
     """q, out [rows, n_heads, head_dim] (rows may lie apart); ``weight`` given: the attention weights are added to it.
     ``scale`` None: 1 / sqrt(head_dim)."""
-    _same_device(k_pages, q, v_pages, table, length, out, workspace, new_start, pos, weight, slopes)
-    kd = _kv_desc(k_pages, v_pages)
-    if out.shape[0] != q.shape[0]:
-        _refuse(ERR_SHAPE, "q and out have different numbers of rows")
-    bd = _kv_batch(kd, table, length, new_start, q.shape[0], max_new, max_len, pos, weight)
-    qp, ldq = _rows(q, None, kd, k_pages.dtype, "q")
-    op, ldo = _rows(out, q.shape[1], kd, k_pages.dtype, "out")
-    ad = AttnDesc(q.shape[1], kd.head_dim ** -0.5 if scale is None else scale, softcap, window,
-                  _typed_ptr(slopes, torch.float32, (q.shape[1],), "slopes"), 0 if weight is None else 1)
-    with _Here(k_pages) as here:
-        _check(lib().llmc_attention_paged(C.byref(kd), C.byref(bd), C.byref(ad), qp, ldq, op, ldo, _ptr(workspace),
-                                          workspace.numel() * workspace.element_size(), here.stream(stream)))
+    dev = k_pages.get_device()
+    kd = _kv_desc(k_pages, v_pages, dev)
+    if len(q.shape) != 3 or out.shape[0] != q.shape[0]:
+        _refuse(ERR_SHAPE, "q and out must be [rows, heads, head_dim] with the same number of rows")
+    n, H, _ = q.shape
+    bd = _kv_batch(kd.page_size, dev, table, length, new_start, n, max_new, max_len, pos, weight)
+    dt, dh = k_pages.dtype, kd.head_dim
+    qp, ldq = _rows(q, H, dh, dt, dev, "q")
+    op, ldo = _rows(out, H, dh, dt, dev, "out")
+    ad = AttnDesc(H, dh ** -0.5 if scale is None else scale, softcap, window,
+                  None if slopes is None else _at(slopes, torch.float32, (H,), dev, "slopes"), 0 if weight is None else 1)
+    ws, nb = _workspace(workspace, dev)
+    _enqueue(lib().llmc_attention_paged, dev, stream, kd, bd, ad, qp, ldq, op, ldo, ws, nb)
 
 
 def llmc_kv_evict_workspace_bytes(table: torch.Tensor, max_len: int) -> int:
@@ -632,22 +625,20 @@ def llmc_kv_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Ten
                   workspace: torch.Tensor, max_len: Optional[int] = None, sink: int = 0, recent: int = 0,
                   stream=None) -> None:
     """Cuts every sequence to its ``keep`` tokens of largest accumulated weight."""
-    _same_device(k_pages, v_pages, table, length, pos, weight, keep, length_out, workspace)
-    kd = _kv_desc(k_pages, v_pages)
-    bd = _kv_batch(kd, table, length, None, 0, 1, max_len, pos, weight)
-    B = table.shape[0]
-    with _Here(k_pages) as here:
-        _check(lib().llmc_kv_evict(C.byref(kd), C.byref(bd), _int_ptr(keep, (B,), "keep"), sink, recent,
-                                   _int_ptr(length_out, (B,), "length_out"), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), here.stream(stream)))
+    dev = k_pages.get_device()
+    kd = _kv_desc(k_pages, v_pages, dev)
+    bd = _kv_batch(kd.page_size, dev, table, length, None, 0, 1, max_len, pos, weight)
+    B = bd.n_seqs
+    kp, lp = _at(keep, torch.int32, (B,), dev, "keep"), _at(length_out, torch.int32, (B,), dev, "length_out")
+    ws, nb = _workspace(workspace, dev)
+    _enqueue(lib().llmc_kv_evict, dev, stream, kd, bd, kp, sink, recent, lp, ws, nb)
 
 
 def llmc_layer_paged_workspace_bytes(layer: Layer, n_rows: int, n_seqs: int, max_new: int, max_len: int,
                                      weights: bool = False) -> int:
-    ld = layer.desc()
     bd = KvBatch(n_seqs, 0, None, None, None, n_rows, max_new, max_len)
     ad = AttnDesc(layer.n_heads, 1.0, 0.0, 0, None, 1 if weights else 0)
-    return lib().llmc_layer_paged_workspace_bytes(C.byref(ld), C.byref(bd), C.byref(ad))
+    return lib().llmc_layer_paged_workspace_bytes(layer.desc(), bd, ad)
 
 
 def llmc_layer_forward_paged(layer: Layer, h_in: torch.Tensor, h_out: torch.Tensor, k_pages: torch.Tensor,
@@ -658,19 +649,17 @@ def llmc_layer_forward_paged(layer: Layer, h_in: torch.Tensor, h_out: torch.Tens
                              window: int = 0, slopes: Optional[torch.Tensor] = None, stream=None) -> None:
     """The decoder block on the new tokens h_in [rows, d]; their keys and values go to the cache.  ``accumulate``: the
     attention weights are added to ``weight``."""
-    _same_device(k_pages, h_in, h_out, v_pages, table, length, workspace, new_start, pos_new, pos, weight, slopes)
-    n, d = h_in.shape
-    kd = _kv_desc(k_pages, v_pages)
-    bd = _kv_batch(kd, table, length, new_start, n, max_new, max_len, pos, weight)
-    ad = AttnDesc(layer.n_heads, kd.head_dim ** -0.5, softcap, window,
-                  _typed_ptr(slopes, torch.float32, (layer.n_heads,), "slopes"), 1 if accumulate else 0)
-    ld = layer.desc()
-    with _Here(k_pages) as here:
-        _check(lib().llmc_layer_forward_paged(C.byref(ld), C.byref(kd), C.byref(bd), C.byref(ad),
-                                              _int_ptr(pos_new, (n,), "pos_new"),
-                                              _typed_ptr(h_in, layer.dtype, (n, layer.d), "h_in"),
-                                              _typed_ptr(h_out, layer.dtype, (n, layer.d), "h_out"), _ptr(workspace),
-                                              workspace.numel() * workspace.element_size(), here.stream(stream)))
+    dev = k_pages.get_device()
+    kd = _kv_desc(k_pages, v_pages, dev)
+    n = h_in.shape[0]
+    bd = _kv_batch(kd.page_size, dev, table, length, new_start, n, max_new, max_len, pos, weight)
+    H = layer.n_heads
+    ad = AttnDesc(H, kd.head_dim ** -0.5, softcap, window,
+                  None if slopes is None else _at(slopes, torch.float32, (H,), dev, "slopes"), 1 if accumulate else 0)
+    pn = None if pos_new is None else _at(pos_new, torch.int32, (n,), dev, "pos_new")
+    hp, op = (_at(t, layer.dtype, (n, layer.d), dev, w) for t, w in ((h_in, "h_in"), (h_out, "h_out")))
+    ws, nb = _workspace(workspace, dev)
+    _enqueue(lib().llmc_layer_forward_paged, dev, stream, layer.desc(), kd, bd, ad, pn, hp, op, ws, nb)
 
 
 def llmc_profile_begin(max_records: int) -> None:

@@ -53,7 +53,7 @@ BAD_BATCH = [
     (None, llmc.ERR_INVALID_ARG), (batch(n_seqs=0), llmc.ERR_INVALID_ARG), (batch(n_seqs=70000), llmc.ERR_SHAPE),
     (batch(max_len=0), llmc.ERR_INVALID_ARG), (batch(max_len=65), llmc.ERR_SHAPE), (batch(max_pages=0), llmc.ERR_SHAPE),
     (batch(max_pages=1 << 28, max_len=1 << 29), llmc.ERR_SHAPE), (batch(d_table=None), llmc.ERR_INVALID_ARG),
-    (batch(d_length=None), llmc.ERR_INVALID_ARG),
+    (batch(d_length=None), llmc.ERR_INVALID_ARG), (batch(d_pos=P + 4), llmc.ERR_SHAPE), (batch(d_weight=P + 8), llmc.ERR_SHAPE),
 ]
 BAD_ROWS = [
     (batch(n_rows=-1), llmc.ERR_INVALID_ARG), (batch(max_new=0), llmc.ERR_INVALID_ARG), (batch(max_new=2), llmc.ERR_SHAPE),
