@@ -37,6 +37,9 @@ struct AttnArgs {
   float* part_o;               // [n_rows * H, n_split, DH], not normalised
   float2* part_ml;             // [n_rows * H, n_split] (maximum in base 2, sum)
   float* lse;                  // [n_rows * H] log2 of the normaliser with the maximum in it, or NULL
+  float* scores;               // [n_seqs, n_kv, join_rows, ld_scores] scores in base 2 of up to 16 rows a head, or NULL
+  int32_t join_rows, ld_scores;
+  int32_t by_length;           // the rows kernel takes the sequences by length
 };
 
 __device__ __forceinline__ float max_over_groups(float v) {      // over the four groups of 16 lanes
@@ -238,22 +241,38 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int blk) {
   return RowBlock{-1, 0};
 }
 
+// The n-th sequence when each group of 64 is ordered by length, longest first.  In the order of the batch, lengths may repeat with the period
+// in which workgroups come back to a compute unit (64 sequences of up to 2048 tokens, 12 heads: 50 us, 42 in order).
+__device__ __forceinline__ int nth_longest(const PagedArgs& p, int n) {
+  const int lane = threadIdx.x & 63, first = n & ~63;
+  const int len = first + lane < p.n_seqs ? p.length[first + lane] : -1;
+  int rank = 0;
+#pragma unroll 8
+  for (int k = 0; k < 64; ++k) {
+    const int other = __builtin_amdgcn_readlane(len, k);
+    rank += other > len || (other == len && k < lane);
+  }
+  return first + __builtin_ctzll(__ballot(rank == n - first));
+}
+
 // ---- few rows, or fp32: keys straight from memory to registers ----------------------------------------------------------
-// A wavefront owns 16 rows and walks the keys in steps of 32 (bf16) or 16 (fp32).  ROWSPLIT 0: the four wavefronts of a
-// workgroup take the same 16 rows and every fourth step, and join their maxima, sums and outputs in LDS: a single token's
-// keys are read once, by as many wavefronts as can be had.  ROWSPLIT 1: they take 64 rows and the same steps.
-template <typename T, int DH, bool FEAT, bool ROWSPLIT>
+// A wavefront owns 16 rows and walks the keys in steps of 32 (bf16) or 16 (fp32), the next step's keys and values in flight
+// while it works on this one's.  ROWSPLIT 0: the four wavefronts of a workgroup take the same 16 rows and every fourth step, and
+// join their maxima, sums and outputs in LDS: a single token's keys are read once.  (8 or 16 wavefronts a workgroup gain nothing: 64
+// sequences of up to 2048 tokens, 12 heads of 64: 48.3 and 55.8 us for 49.9; one of 777: 8.5 and 10.2 for 8.0.)
+// ROWSPLIT 1: they take 64 rows and the same steps.
+// FEAT 0: plain scores, 1: capped, biased or in a window, 2: the same with positions that are not the slots.
+template <typename T, int DH, int FEAT, bool ROWSPLIT>
 __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   typedef Frag<T, DH> F;
   typedef typename F::E E;
-  constexpr int NV = F::NV, SUB = F::SUB, KEYS = F::KEYS, ROWS = ROWSPLIT ? 64 : 16, LDO = DH + 4;
-  constexpr int STEP = ROWSPLIT ? KEYS : 4 * KEYS;
-  __shared__ __attribute__((aligned(16))) float sO[ROWSPLIT ? 4 : 4 * 16 * LDO];
-  __shared__ float sM[4][16], sL[4][16];
+  constexpr int NW = 4, NV = F::NV, SUB = F::SUB, KEYS = F::KEYS, ROWS = ROWSPLIT ? 16 * NW : 16, LDO = DH + 4;
+  constexpr int STEP = ROWSPLIT ? KEYS : NW * KEYS;
+  extern __shared__ __attribute__((aligned(16))) float rows_lds[];          // ROWSPLIT 0: [NW][join_rows][LDO], then maxima, sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int piece = blockIdx.x % a.n_split, unit = blockIdx.x / a.n_split;
-  const int h = unit % a.p.n_kv;
-  const RowBlock rb = row_block<ROWS>(a, unit / a.p.n_kv);
+  const int h = blockIdx.x % a.p.n_kv, piece = blockIdx.x / a.p.n_kv % a.n_split;
+  const int unit = blockIdx.x / a.p.n_kv / a.n_split;
+  const RowBlock rb = ROWSPLIT ? row_block<ROWS>(a, unit) : RowBlock{a.by_length ? nth_longest(a.p, unit) : unit, 0};
   if (rb.b < 0) return;
   const SeqRange s = seq_range(a.p, rb.b);
   const int rows = s.q * a.G;
@@ -270,14 +289,14 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   const int row = s.first + i_new, t_slot = s.len - s.q + i_new;
   const int t_first = s.len - s.q + m0 / a.G;                   // the first row's slot: all rows see the keys up to it
   if (ROWSPLIT) k_hi = min(k_hi, max(0, s.len - s.q + min((m0 + 15) / a.G, s.q - 1) + 1));
-  const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)rb.b * a.p.max_pages << a.p.page_shift) : nullptr;
+  const int slots = a.p.max_pages << a.p.page_shift;
+  const int32_t* pos = FEAT == 2 ? a.pos + (size_t)rb.b * slots : nullptr;
   float slope = 0.f;
   int t_pos = t_slot;
   if (FEAT) {
     if (a.slopes) slope = a.slopes[head] * kLog2e;
-    if (pos && t_slot >= 0) t_pos = pos[t_slot];
+    if (FEAT == 2 && t_slot >= 0) t_pos = pos[t_slot];
   }
-  const int slots = a.p.max_pages << a.p.page_shift;
   typename F::Q fq;
   F::load_q(fq, (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
   f32x4_t o[NV];
@@ -285,36 +304,56 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   for (int t = 0; t < NV; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
   const int page_mask = (1 << a.p.page_shift) - 1;
+  // scores of these rows, for the weights that the keys receive
+  float* score = a.scores && row_there ? a.scores + (((size_t)rb.b * a.p.n_kv + h) * a.join_rows + mc) * a.ld_scores + 4 * g : nullptr;
 
-  for (int kb = k_lo + (ROWSPLIT ? 0 : wave * KEYS); kb < k_hi; kb += STEP) {
-    typename F::K fk;
-    typename F::V fv;
-    bool no_page[SUB];
+  // A step's keys and values.  Pages are scalar loads, so waiting for them waits for no other load in flight; they are asked for one
+  // step earlier than the keys.  Beyond the last step the last one is read again (a conditional load would have to be waited for
+  // together with what is in flight).
+  struct Step {
+    typename F::K k;
+    typename F::V v;
+    int4 pos[SUB];
+    int page[SUB];
+  };
+  typedef const __attribute__((address_space(4))) int32_t scalar_i32;
+  scalar_i32* table = (scalar_i32*)(uintptr_t)(a.p.table + (size_t)rb.b * a.p.max_pages);
+  const int k_first = k_lo + (ROWSPLIT ? 0 : wave * KEYS);
+  const int k_last = k_first + max(0, k_hi - 1 - k_first) / STEP * STEP;     // this wavefront's last step
+  int page_next[SUB];
+  auto ask_pages = [&](int kb) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+      page_next[u] = table[min((min(kb, k_last) + 16 * u) >> a.p.page_shift, a.p.max_pages - 1)];
+  };
+  auto fetch = [&](Step& st, int kb) {
+    kb = min(kb, k_last);
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
-      const int page = page_of(a.p, rb.b, kb + 16 * u);
-      no_page[u] = page < 0;
-      const size_t at = ((((size_t)max(page, 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
-      F::load_k(fk, u, (const E*)a.k + at, c, g);
-      F::load_v(fv, u, (const E*)a.v + at, c, g);
+      st.page[u] = (uint32_t)page_next[u] < (uint32_t)a.p.n_pages ? page_next[u] : -1;
+      const size_t at = ((((size_t)max(st.page[u], 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
+      F::load_k(st.k, u, (const E*)a.k + at, c, g);
+      F::load_v(st.v, u, (const E*)a.v + at, c, g);
+      if (FEAT == 2) st.pos[u] = reinterpret_cast<const int4*>(pos)[min(kb + 16 * u + 4 * g, slots - 4) >> 2];
     }
+  };
+  auto work = [&](Step& st, int kb) {
     float x[SUB * 4];
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
-      const f32x4_t sc = F::qk(fk, u, fq);
+      const f32x4_t sc = F::qk(st.k, u, fq);
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[u * 4 + r] = sc[r];
     }
     bool edge = kb + KEYS - 1 > t_first || kb + KEYS > s.len;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) edge |= no_page[u];
+    for (int u = 0; u < SUB; ++u) edge |= st.page[u] < 0;
     if (FEAT) {
-      const int4* kp = reinterpret_cast<const int4*>(pos);
       int key_pos[SUB * 4];
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         const int key0 = kb + 16 * u + 4 * g;
-        const int4 v = pos ? kp[min(key0, slots - 4) >> 2] : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
+        const int4 v = FEAT == 2 ? st.pos[u] : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
         key_pos[u * 4] = v.x; key_pos[u * 4 + 1] = v.y; key_pos[u * 4 + 2] = v.z; key_pos[u * 4 + 3] = v.w;
       }
       transform(a, x, [&](int i) { return key_pos[i]; }, slope, t_pos);
@@ -328,10 +367,16 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int key = kb + 16 * u + 4 * g + r;
-          if (key > t_slot || no_page[u]) x[u * 4 + r] = -INFINITY;
+          if (key > t_slot || st.page[u] < 0) x[u * 4 + r] = -INFINITY;
           // what lies behind the sequence in its last page may be anything, and 0 * anything is not always 0
-          if (key >= s.len || no_page[u]) F::clear_v(fv, u, r);
+          if (key >= s.len || st.page[u] < 0) F::clear_v(st.v, u, r);
         }
+    }
+    if (!ROWSPLIT && score) {
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+        if (kb + 16 * u < k_hi)
+          *reinterpret_cast<float4*>(score + kb + 16 * u) = make_float4(x[u * 4], x[u * 4 + 1], x[u * 4 + 2], x[u * 4 + 3]);
     }
     float mx = x[0];
 #pragma unroll
@@ -353,7 +398,25 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
       pr[i >> 2][i & 3] = __builtin_amdgcn_exp2f(x[i] - m_use);
       l_run += pr[i >> 2][i & 3];
     }
-    F::pv(fv, pr, o);
+    F::pv(st.v, pr, o);
+  };
+  if (k_first < k_hi) {
+    Step s0, s1;
+    ask_pages(k_first);
+    fetch(s0, k_first);
+    ask_pages(k_first + STEP);
+    for (int kb = k_first;;) {
+      fetch(s1, kb + STEP);
+      ask_pages(kb + 2 * STEP);
+      work(s0, kb);
+      kb += STEP;
+      if (kb >= k_hi) break;
+      fetch(s0, kb + STEP);
+      ask_pages(kb + 2 * STEP);
+      work(s1, kb);
+      kb += STEP;
+      if (kb >= k_hi) break;
+    }
   }
   l_run = sum_over_groups(l_run);
 
@@ -383,61 +446,51 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     }
     return;
   }
+  const int R = a.join_rows;                                     // at least as many as this block has
+  float* sM = rows_lds + NW * R * LDO;
+  float* sL = sM + NW * R;
+  if (c < R) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    float y[NV];
+    for (int r = 0; r < 4; ++r) {
+      float y[NV];
 #pragma unroll
-    for (int t = 0; t < NV; ++t) y[t] = o[t][r];
-    store_vec<float, NV>(&sO[(wave * 16 + c) * LDO + (4 * g + r) * NV], y);
+      for (int t = 0; t < NV; ++t) y[t] = o[t][r];
+      store_vec<float, NV>(&rows_lds[(wave * R + c) * LDO + (4 * g + r) * NV], y);
+    }
+    if (g == 0) { sM[wave * R + c] = m_run; sL[wave * R + c] = l_run; }
   }
-  if (g == 0) { sM[wave][c] = m_run; sL[wave][c] = l_run; }
   __syncthreads();
-  // joined by 16 threads a row, NV dims each
-  const int jr = threadIdx.x >> 4, jd = (threadIdx.x & 15) * NV, jm = rb.mb * ROWS + jr;
-  if (jm >= rows) return;
-  float top = sM[0][jr];
+  // joined by a thread a row and dim
+  for (int e = threadIdx.x; e < rows * DH; e += NW * 64) {
+    const int jr = e / DH, jd = e % DH;
+    float top = -INFINITY;
 #pragma unroll
-  for (int w = 1; w < 4; ++w) top = fmaxf(top, sM[w][jr]);
-  const float top_use = top == -INFINITY ? 0.f : top;
-  float l = 0.f, y[NV];
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, sM[w * R + jr]);
+    const float top_use = top == -INFINITY ? 0.f : top;
+    float l = 0.f, y = 0.f;
 #pragma unroll
-  for (int t = 0; t < NV; ++t) y[t] = 0.f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = __builtin_amdgcn_exp2f(sM[w][jr] - top_use);
-    l += f * sL[w][jr];
-#pragma unroll
-    for (int t = 0; t < NV; ++t) y[t] += f * sO[(w * 16 + jr) * LDO + jd + t];
-  }
-  const int jrow = s.first + jm / a.G, jhead = h * a.G + jm % a.G;
-  const size_t rh = (size_t)jrow * a.H + jhead;
-  if (n_pieces == 1) {
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-#pragma unroll
-    for (int t = 0; t < NV; ++t) y[t] *= inv;
-    store_vec<T, NV>((T*)a.out + (size_t)jrow * a.ld_out + jhead * DH + jd, y);
-    if (a.lse && jd == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
-  } else {
-    store_vec<float, NV>(a.part_o + (rh * a.n_split + piece) * DH + jd, y);
-    if (jd == 0) a.part_ml[rh * a.n_split + piece] = make_float2(top, l);
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sM[w * R + jr] - top_use);
+      l += f * sL[w * R + jr];
+      y += f * rows_lds[(w * R + jr) * LDO + jd];
+    }
+    const int jrow = s.first + jr / a.G, jhead = h * a.G + jr % a.G;
+    const size_t rh = (size_t)jrow * a.H + jhead;
+    if (n_pieces == 1) {
+      Elem<T>::store((T*)a.out + (size_t)jrow * a.ld_out + jhead * DH + jd, y * (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l)));
+      if (a.lse && jd == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
+    } else {
+      a.part_o[(rh * a.n_split + piece) * DH + jd] = y;
+      if (jd == 0) a.part_ml[rh * a.n_split + piece] = make_float2(top, l);
+    }
   }
 }
 
 // ---- the pieces of a long axis joined: a wavefront a (row, head) -------------------------------------------------------
-template <typename T, int DH, int ROWS>
-__global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
-  const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (rh >= (int64_t)a.p.n_rows * a.H) return;
-  const int lane = threadIdx.x & 63, row = (int)(rh / a.H), head = (int)(rh % a.H);
-  const int b = seq_of_row(a.p, row);
-  if (b < 0) return;
-  const SeqRange s = seq_range(a.p, b);
-  const int i = row - s.first;
-  if (i >= s.q) return;
-  const int m = i * a.G + head % a.G;
-  const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
-  const int n = max(1, (kr.hi - kr.lo + a.split - 1) / a.split);
-  if (n == 1) return;                                            // written where it was computed
+template <typename T, int DH>
+__device__ __forceinline__ void join_pieces(const AttnArgs& a, int row, int head, int n) {
+  const int lane = threadIdx.x & 63;
+  const size_t rh = (size_t)row * a.H + head;
   const float2* ml = a.part_ml + rh * a.n_split;
   const float* po = a.part_o + rh * a.n_split * DH;
   float top = -INFINITY;
@@ -449,7 +502,7 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   float l = 0.f, y[PER];
 #pragma unroll
   for (int t = 0; t < PER; ++t) y[t] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
   for (int j = 0; j < n; ++j) {
     const float2 v = ml[j];
     const float f = __builtin_amdgcn_exp2f(v.x - top_use);
@@ -462,6 +515,22 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   for (int t = 0; t < PER; ++t)
     Elem<T>::store((T*)a.out + (size_t)row * a.ld_out + head * DH + t * 64 + lane, y[t] * inv);
   if (a.lse && lane == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
+}
+
+template <typename T, int DH, int ROWS>
+__global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
+  const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (rh >= (int64_t)a.p.n_rows * a.H) return;
+  const int row = (int)(rh / a.H), head = (int)(rh % a.H);
+  const int b = seq_of_row(a.p, row);
+  if (b < 0) return;
+  const SeqRange s = seq_range(a.p, b);
+  const int i = row - s.first;
+  if (i >= s.q) return;
+  const int m = i * a.G + head % a.G;
+  const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
+  const int n = (kr.hi - kr.lo + a.split - 1) / a.split;
+  if (n > 1) join_pieces<T, DH>(a, row, head, n);               // else written where it was computed
 }
 
 // ---- many rows in bf16: 128 rows a workgroup share key tiles in LDS -----------------------------------------------------
@@ -515,7 +584,7 @@ __device__ __forceinline__ uint2 lds_read_transposed(const uint16_t* p) {
   return __builtin_bit_cast(uint2, lds_read_tr((lds_v4s16_t*)p));
 }
 
-template <int DH, bool FEAT>
+template <int DH, int FEAT>
 __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_kernel(AttnArgs a) {
   typedef TileCfg<DH> C;
   constexpr int NF = DH / 32, KS = DH / 16;
@@ -540,16 +609,16 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
   const int row = s.first + i_new, t_slot = s.len - s.q + i_new;
   const int t_first = s.len - s.q + m0 / a.G;
   const int t_last = s.len - s.q + min((m0 + 31) / a.G, s.q - 1);
-  const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)rb.b * a.p.max_pages << a.p.page_shift) : nullptr;
+  const int slots = a.p.max_pages << a.p.page_shift;
+  const int32_t* pos = FEAT == 2 ? a.pos + (size_t)rb.b * slots : nullptr;
   float slope = 0.f;
   int t_pos = t_slot;
   if (FEAT) {
     if (a.slopes) slope = a.slopes[head] * kLog2e;
-    if (pos && t_slot >= 0) t_pos = pos[t_slot];
+    if (FEAT == 2 && t_slot >= 0) t_pos = pos[t_slot];
   }
 
   PageWindow pages(a.p, rb.b, k_lo >> a.p.page_shift);
-  const int slots = a.p.max_pages << a.p.page_shift;
   const int page_mask = (1 << a.p.page_shift) - 1;
   // this lane's row and chunk in a load instruction; the swizzle looks at rows modulo 16, so it differs between instructions
   const int ld_row = lane / C::CH, ld_slot = lane % C::CH;
@@ -559,7 +628,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
     bad_next = false;
     for (int col = kb >> a.p.page_shift; col <= (min(kb + C::KT, s.len) - 1) >> a.p.page_shift; ++col)
       bad_next |= pages.at(col) < 0;
-    if (FEAT && pos && wave == 3)
+    if (FEAT == 2 && wave == 3)
       __builtin_amdgcn_global_load_lds(LLMC_GPTR(pos + min(kb + lane, slots - 1)),
                                        LLMC_LPTR(tile_lds + 4 * C::TILE + buf * 2 * C::KT), 4, 0, 0);
 #pragma unroll
@@ -628,7 +697,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
     const int key0 = kb + half * 4;
     if (FEAT) {
       const int* tile_pos = reinterpret_cast<const int*>(tile_lds + 4 * C::TILE + buf * 2 * C::KT) + half * 4;
-      transform(a, x, [&](int i) { return pos ? tile_pos[off(i)] : key0 + off(i); }, slope, t_pos);
+      transform(a, x, [&](int i) { return FEAT == 2 ? tile_pos[off(i)] : key0 + off(i); }, slope, t_pos);
     }
     if (kb + C::KT - 1 > t_first) {
 #pragma unroll
@@ -728,7 +797,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
 // ascending order by the second kernel: no atomics, one order.
 constexpr int kWeightKeys = 256;                                 // a workgroup
 
-template <typename T, int DH, bool FEAT>
+template <typename T, int DH, int FEAT>
 __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a, float* __restrict__ sums) {
   typedef Frag<T, DH> F;
   typedef typename F::E E;
@@ -740,7 +809,7 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
   const int kb = blk * kWeightKeys + wave * 64;
   if (kb >= s.len) return;
   const int slots = a.p.max_pages << a.p.page_shift;
-  const int32_t* pos = FEAT && a.pos ? a.pos + ((size_t)b * a.p.max_pages << a.p.page_shift) : nullptr;
+  const int32_t* pos = FEAT == 2 ? a.pos + (size_t)b * slots : nullptr;
   const int page_mask = (1 << a.p.page_shift) - 1;
   typename F::K fk[NK];
   bool no_page[4];
@@ -771,7 +840,7 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
     int t_pos = t_slot;
     if (FEAT) {
       if (a.slopes) slope = a.slopes[head] * kLog2e;
-      if (pos && t_slot >= 0) t_pos = pos[t_slot];
+      if (FEAT == 2 && t_slot >= 0) t_pos = pos[t_slot];
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -781,7 +850,7 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[r] = sc[r];
       if (FEAT) {
-        const int4 v = pos ? reinterpret_cast<const int4*>(pos)[min(key0, slots - 4) >> 2]
+        const int4 v = FEAT == 2 ? reinterpret_cast<const int4*>(pos)[min(key0, slots - 4) >> 2]
                            : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
         const int key_pos[4] = {v.x, v.y, v.z, v.w};
         transform(a, x, [&](int i) { return key_pos[i]; }, slope, t_pos);
@@ -828,10 +897,77 @@ __global__ __launch_bounds__(256) void attention_paged_add_weights_kernel(PagedA
   weight[((size_t)b * p.max_pages << p.page_shift) + key] += v;
 }
 
+// The same from the scores that the attention itself left, for calls of up to 16 rows a head.  A workgroup takes 256 keys, four a
+// lane; its wavefronts take a quarter of the rows of all heads each, and the four sums are added in order: the loads of a
+// thread are few and independent, which is what this is bound by.  Keys outside the rows' range have no scores.  Where the key
+// axis was cut, the normalisers are made from the pieces' here, and workgroups beyond the keys' join the outputs (a launch
+// of their own takes 7 us for 6 sequences of up to 32768 tokens).
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void attention_paged_score_weights_kernel(AttnArgs a, float* __restrict__ weight, int n_kb) {
+  __shared__ float4 part[3][64];
+  const int b = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const SeqRange s = seq_range(a.p, b);
+  const int rows = s.q * a.G, n = a.p.n_kv * rows;
+  if (rows == 0) return;
+  const KeyRange kr = key_range(a, s, 0, 16);                    // lo is a multiple of 64
+  const int n_pieces = (kr.hi - kr.lo + a.split - 1) / a.split;
+  if ((int)blockIdx.x >= n_kb) {
+    const int r = ((int)blockIdx.x - n_kb) * 4 + wave, h = r / rows, m = r - h * rows;
+    if (r < n && n_pieces > 1) join_pieces<T, DH>(a, s.first + m / a.G, h * a.G + m % a.G, n_pieces);
+    return;
+  }
+  const int key = blockIdx.x * 256 + lane * 4;
+  if ((int)blockIdx.x * 256 >= kr.hi || (int)blockIdx.x * 256 + 256 <= kr.lo) return;
+  const bool there = key >= kr.lo && key < kr.hi;
+  const int per = (n + 3) / 4, r0 = wave * per, r1 = min(n, r0 + per);
+  const float* src = a.scores + (size_t)b * a.p.n_kv * a.join_rows * a.ld_scores + (there ? key : kr.lo);
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int r = r0; r < r1; ++r) {
+    const int h = r / rows, m = r - h * rows;
+    const float4 x = *reinterpret_cast<const float4*>(src + ((size_t)h * a.join_rows + m) * a.ld_scores);
+    const size_t rh = (size_t)(s.first + m / a.G) * a.H + h * a.G + m % a.G;
+    float lse;
+    if (n_pieces > 1) {
+      const float2* ml = a.part_ml + rh * a.n_split;
+      float top = -INFINITY, l = 0.f;
+      for (int j = lane; j < n_pieces; j += 64) {
+        const float2 v = ml[j];
+        const float t = fmaxf(top, v.x), t_use = t == -INFINITY ? 0.f : t;
+        l = l * __builtin_amdgcn_exp2f(top - t_use) + v.y * __builtin_amdgcn_exp2f(v.x - t_use);
+        top = t;
+      }
+      float all = top;
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+      const float all_use = all == -INFINITY ? 0.f : all;
+      l = wave_sum(l * __builtin_amdgcn_exp2f(top - all_use));
+      lse = l == 0.f ? INFINITY : all + __builtin_amdgcn_logf(l);
+    } else {
+      lse = a.lse[rh];
+    }
+    const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] += xs[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(xs[i] - lse);
+  }
+  if (wave > 0) part[wave - 1][lane] = make_float4(w[0], w[1], w[2], w[3]);
+  __syncthreads();
+  if (wave > 0 || !there) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const float4 v = part[i][lane];
+    w[0] += v.x; w[1] += v.y; w[2] += v.z; w[3] += v.w;
+  }
+  float* dst = weight + ((size_t)b * a.p.max_pages << a.p.page_shift) + key;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (key + i < kr.hi) dst[i] += w[i];
+}
+
 // ---- host ---------------------------------------------------------------------------------------------------------------
 struct Plan {
   bool tile, rowsplit;
   int rows;                    // of a row block
+  int join_rows;               // rows a head at most, where a workgroup's wavefronts are joined
   int64_t blocks;              // row blocks of all sequences, at most
   int split, n_split;
 };
@@ -845,50 +981,63 @@ Plan make_plan(int dtype, int n_rows, int n_seqs, int n_kv, int G, int max_new, 
   p.tile = rows > 16 && dtype == LLMC_BF16;
   p.rowsplit = rows > 16 && !p.tile;
   p.rows = p.tile ? 128 : p.rowsplit ? 64 : 16;
+  p.join_rows = (int)std::min<int64_t>(rows, 16);
   p.blocks = rows <= p.rows ? n_seqs : std::min<int64_t>((rows + p.rows - 1) / p.rows * n_seqs, (int64_t)n_rows * G / p.rows + n_seqs);
-  const int64_t target = p.tile ? 512 : 1024;                    // workgroups that the chip holds at once
   const int64_t units = std::max<int64_t>(1, p.blocks * n_kv);
-  const int64_t want = std::max<int64_t>(1, target / units);
+  int64_t want;                // pieces of the key axis
+  if (p.tile || p.rowsplit) {
+    want = (p.tile ? 512 : 1024) / units;
+  } else {
+    // Eight steps of a workgroup take as long as the second launch that joins pieces (one sequence of 777 tokens, 12 heads of 64: 8.0 us
+    // in one piece, 4.4 + 4.0 in seven).  From two workgroups a compute unit on, cutting gains less than that launch (64 sequences
+    // of up to 2048: 42 and 47 + 4); below, pieces even out ragged lengths (6 of up to 32768, 8 heads of 128: 1024 workgroups
+    // 106 + 4.5 us, 2048 92 + 7, 4096 93 + 10).
+    const int steps8 = 8 * 4 * (dtype == LLMC_BF16 ? 32 : 16);
+    want = max_len <= steps8 || units >= 512 ? 1 : 2048 / units;
+  }
+  want = std::max<int64_t>(1, want);
   p.split = (int)std::max<int64_t>(256, align_up((size_t)((max_len + want - 1) / want), 128));
   p.n_split = std::max(1, (int)((max_len + p.split - 1) / p.split));
   return p;
 }
 
-struct Layout { size_t part_o, part_ml, lse, sums, total; };
+struct Layout { size_t part_o, part_ml, lse, scores, sums, total; int ld_scores; };
 Layout ws_layout(const Plan& p, int n_rows, int H, int DH, int n_seqs, int n_kv, int max_len, bool weights) {
   Layout l{};
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes, 256); return r; };
   const size_t rh = (size_t)n_rows * H;
+  const bool scores = weights && !p.tile && !p.rowsplit;
+  l.ld_scores = (int)align_up((size_t)max_len, 16);
   l.part_o = take(p.n_split > 1 ? rh * p.n_split * DH * 4 : 0);
   l.part_ml = take(p.n_split > 1 ? rh * p.n_split * 8 : 0);
   l.lse = take(weights ? rh * 4 : 0);
-  l.sums = take(weights ? (size_t)n_seqs * n_kv * max_len * 4 : 0);
+  l.scores = take(scores ? (size_t)n_seqs * n_kv * p.join_rows * l.ld_scores * 4 : 0);
+  l.sums = take(weights && !scores ? (size_t)n_seqs * n_kv * max_len * 4 : 0);
   l.total = std::max<size_t>(at, 256);
   return l;
 }
 
-template <typename T, int DH, bool FEAT>
+template <typename T, int DH, int FEAT>
 llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* weight, hipStream_t st) {
   const unsigned grid = (unsigned)(p.blocks * a.p.n_kv * p.n_split);
   {
     ProfScope ps_("attention_paged_kernel", st);
-    if constexpr (sizeof(T) == 2) {
-      if (p.tile) {
-        static std::atomic<bool> lds_set[64];
-        const auto kernel = attention_paged_tile_kernel<DH, FEAT>;
-        LLMC_TRY(ensure_dynamic_lds((const void*)kernel, TileCfg<DH>::LDS_BYTES, lds_set));
-        LLMC_KERNEL_GGL(kernel, dim3(grid), dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
-      } else {
-        LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), 0, st, a);
-      }
+    if (!p.tile && !p.rowsplit) {
+      // 16 rows of 128 dims take 33.8 KiB: no more than a kernel may have without asking
+      const size_t lds = (size_t)4 * p.join_rows * (DH + 4 + 2) * 4;
+      LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), lds, st, a);
+    } else if constexpr (sizeof(T) == 2) {
+      static std::atomic<bool> lds_set[64];
+      const auto kernel = attention_paged_tile_kernel<DH, FEAT>;
+      LLMC_TRY(ensure_dynamic_lds((const void*)kernel, TileCfg<DH>::LDS_BYTES, lds_set));
+      LLMC_KERNEL_GGL(kernel, dim3(grid), dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
     } else {
-      if (p.rowsplit) LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), dim3(grid), dim3(256), 0, st, a);
-      else LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), 0, st, a);
+      LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), dim3(grid), dim3(256), 0, st, a);
     }
   }
   LLMC_LAUNCH_CHECK("attention_paged");
-  if (p.n_split > 1) {
+  if (p.n_split > 1 && !a.scores) {
     ProfScope ps_("attention_paged_join_kernel", st);
     const dim3 jg((unsigned)(((int64_t)a.p.n_rows * a.H + 3) / 4));
     if (p.rows == 128) LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 128>), jg, dim3(256), 0, st, a);
@@ -896,7 +1045,13 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
     else LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 16>), jg, dim3(256), 0, st, a);
     LLMC_LAUNCH_CHECK("attention_paged_join");
   }
-  if (weight) {
+  if (weight && a.scores) {
+    { ProfScope ps_("attention_paged_weight_kernel", st);
+      const int n_kb = (a.p.max_len + 255) / 256, n_join = p.n_split > 1 ? (p.join_rows * a.p.n_kv + 3) / 4 : 0;
+      LLMC_KERNEL_GGL((attention_paged_score_weights_kernel<T, DH>), dim3(n_kb + n_join, a.p.n_seqs), dim3(256), 0, st, a, weight,
+                      n_kb); }
+    LLMC_LAUNCH_CHECK("attention_paged_score_weights");
+  } else if (weight) {
     const int n_kb = (a.p.max_len + kWeightKeys - 1) / kWeightKeys;
     { ProfScope ps_("attention_paged_weight_kernel", st);
       LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), dim3((unsigned)((int64_t)n_kb * a.p.n_kv * a.p.n_seqs)),
@@ -943,11 +1098,16 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   char* w = (char*)ws;
   a.part_o = (float*)(w + l.part_o); a.part_ml = (float2*)(w + l.part_ml);
   a.lse = weights ? (float*)(w + l.lse) : nullptr;
+  a.by_length = bt->n_seqs > 1 && p.blocks * kv->n_kv_heads * p.n_split > 256;
+  a.join_rows = p.join_rows; a.ld_scores = l.ld_scores;
+  a.scores = weights && !p.tile && !p.rowsplit ? (float*)(w + l.scores) : nullptr;
   float* sums = weights ? (float*)(w + l.sums) : nullptr;
   float* weight = weights ? bt->d_weight : nullptr;
-  const bool feat = at->softcap > 0.f || at->window > 0 || at->d_slopes;
-#define LLMC_PAGED(T_, DH_) \
-  return feat ? launch_t<T_, DH_, true>(a, p, sums, weight, st) : launch_t<T_, DH_, false>(a, p, sums, weight, st)
+  const int feat = a.pos ? 2 : at->softcap > 0.f || at->window > 0 || at->d_slopes ? 1 : 0;
+#define LLMC_PAGED(T_, DH_)                                                  \
+  return feat == 2   ? launch_t<T_, DH_, 2>(a, p, sums, weight, st)          \
+         : feat == 1 ? launch_t<T_, DH_, 1>(a, p, sums, weight, st)          \
+                     : launch_t<T_, DH_, 0>(a, p, sums, weight, st)
   if (kv->dtype == LLMC_BF16) {
     if (kv->head_dim == 64) LLMC_PAGED(bf16_t, 64);
     LLMC_PAGED(bf16_t, 128);
