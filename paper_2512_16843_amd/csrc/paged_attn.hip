@@ -17,7 +17,11 @@
 namespace llmc {
 namespace {
 
+typedef const __attribute__((address_space(4))) int32_t scalar_i32;    // read through the scalar cache
 constexpr float kLog2e = 1.4426950408889634f;
+// The maximum that a row's sums count from follows its scores only where they outgrow it by this much in base 2: weights up to
+// 2^8 are as good as weights up to one in floating point, and most steps then rescale nothing.
+constexpr float kSlack = 8.f;
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 struct AttnArgs {
@@ -27,8 +31,9 @@ struct AttnArgs {
   const void *k, *v;
   int64_t ld_q, ld_out;
   int32_t H, G;
-  float scale2, softcap;       // scale * log2(e)
-  float cap_in, cap_out;       // scale * 2 log2(e) / softcap, softcap * log2(e)
+  float softcap;
+  float mul, add;              // a score in base 2 from a product (scale * log2(e), 0) or, capped, from y (2 c, c; c = softcap * log2(e))
+  float cap_in;                // scale * 2 log2(e) / softcap
   int32_t window;              // 0: none
   const float* slopes;
   const int32_t* pos;          // NULL: slots are positions
@@ -69,31 +74,25 @@ __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, const SeqRange&
   return r;
 }
 
-// Scores in base 2 from N products; at(i) is the position of the i-th key.  The branches are uniform and outside the loops.
-//   capped: c (1 - 2 / (1 + 2^(x 2 log2(e) / c))), one exponential and one reciprocal, exact at both ends
-template <int N, typename At>
-__device__ __forceinline__ void transform(const AttnArgs& a, float (&x)[N], At at, float slope2, int t_pos) {
-  if (a.softcap > 0.f) {
+// A capped score in base 2 is c + 2 c y with y = -1 / (1 + 2^(2 log2(e) x / c)): one exponential and one reciprocal, exact at
+// both ends, and y takes the place of the product in the one fma of the exponent.
+template <int N>
+__device__ __forceinline__ void cap_scores(const AttnArgs& a, float (&y)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float e = __builtin_amdgcn_exp2f(x[i] * a.cap_in);
-      x[i] = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + e), a.cap_out);
-    }
-  } else {
+  for (int i = 0; i < N; ++i) y[i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(y[i] * a.cap_in));
+}
+
+// Scores in base 2 from N products, lowered by slope2 * away(i) and hidden at and beyond the window.  The branches are uniform
+// and outside the loops.
+template <int N, typename Away>
+__device__ __forceinline__ void bias_scores(const AttnArgs& a, float (&x)[N], Away away, float slope2) {
+  if (a.softcap > 0.f) cap_scores(a, x);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] *= a.scale2;
-  }
-  if (a.slopes || a.window > 0) {
-    int away[N];
+  for (int i = 0; i < N; ++i) x[i] = fmaf(-slope2, (float)away(i), fmaf(x[i], a.mul, a.add));
+  if (a.window > 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) away[i] = t_pos - at(i);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = fmaf(-slope2, (float)away[i], x[i]);
-    if (a.window > 0) {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (away[i] >= a.window) x[i] = -INFINITY;
-    }
+    for (int i = 0; i < N; ++i)
+      if (away(i) >= a.window) x[i] = -INFINITY;
   }
 }
 
@@ -261,7 +260,7 @@ __device__ __forceinline__ int nth_longest(const PagedArgs& p, int n) {
 // join their maxima, sums and outputs in LDS: a single token's keys are read once.  (8 or 16 wavefronts a workgroup gain nothing: 64
 // sequences of up to 2048 tokens, 12 heads of 64: 48.3 and 55.8 us for 49.9; one of 777: 8.5 and 10.2 for 8.0.)
 // ROWSPLIT 1: they take 64 rows and the same steps.
-// FEAT 0: plain scores, 1: capped, biased or in a window, 2: the same with positions that are not the slots.
+// FEAT 0: plain scores, 1: capped, biased or in a window, 2: the same with positions that are not the slots' numbers.
 template <typename T, int DH, int FEAT, bool ROWSPLIT>
 __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   typedef Frag<T, DH> F;
@@ -316,7 +315,6 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     int4 pos[SUB];
     int page[SUB];
   };
-  typedef const __attribute__((address_space(4))) int32_t scalar_i32;
   scalar_i32* table = (scalar_i32*)(uintptr_t)(a.p.table + (size_t)rb.b * a.p.max_pages);
   const int k_first = k_lo + (ROWSPLIT ? 0 : wave * KEYS);
   const int k_last = k_first + max(0, k_hi - 1 - k_first) / STEP * STEP;     // this wavefront's last step
@@ -348,18 +346,16 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     bool edge = kb + KEYS - 1 > t_first || kb + KEYS > s.len;
 #pragma unroll
     for (int u = 0; u < SUB; ++u) edge |= st.page[u] < 0;
-    if (FEAT) {
-      int key_pos[SUB * 4];
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        const int key0 = kb + 16 * u + 4 * g;
-        const int4 v = FEAT == 2 ? st.pos[u] : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
-        key_pos[u * 4] = v.x; key_pos[u * 4 + 1] = v.y; key_pos[u * 4 + 2] = v.z; key_pos[u * 4 + 3] = v.w;
-      }
-      transform(a, x, [&](int i) { return key_pos[i]; }, slope, t_pos);
+    if (FEAT == 2) {
+      const int key_pos[8] = {st.pos[0].x, st.pos[0].y, st.pos[0].z, st.pos[0].w, st.pos[SUB - 1].x, st.pos[SUB - 1].y,
+                              st.pos[SUB - 1].z, st.pos[SUB - 1].w};
+      bias_scores(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
+    } else if (FEAT == 1) {
+      const int away0 = t_slot - kb - 4 * g;
+      bias_scores(a, x, [&](int i) { return away0 - 16 * (i >> 2) - (i & 3); }, slope);
     } else {
 #pragma unroll
-      for (int i = 0; i < SUB * 4; ++i) x[i] *= a.scale2;
+      for (int i = 0; i < SUB * 4; ++i) x[i] *= a.mul;
     }
     if (edge) {
 #pragma unroll
@@ -381,17 +377,17 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < SUB * 4; ++i) mx = fmaxf(mx, x[i]);
-    const float m_new = fmaxf(m_run, max_over_groups(mx));
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;        // a row that has seen no key so far
-    if (__any(m_new > m_run)) {
-      const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+    const float m_new = max_over_groups(mx);
+    if (__any(m_new > m_run + kSlack)) {
+      const float m_top = fmaxf(m_run, m_new), corr = m_top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_top);
+      m_run = m_top;
       l_run *= corr;
 #pragma unroll
       for (int t = 0; t < NV; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[t][r] *= corr;
     }
-    m_run = m_new;
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;        // a row that has seen no key so far
     float pr[SUB][4];
 #pragma unroll
     for (int i = 0; i < SUB * 4; ++i) {
@@ -534,44 +530,26 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
 }
 
 // ---- many rows in bf16: 128 rows a workgroup share key tiles in LDS -----------------------------------------------------
-// Four wavefronts of 32 rows, tiles of 64 keys and values, double buffered, filled by direct global -> LDS loads: a load
-// instruction of a wavefront fills 1 KiB, rows of one page, so its page is a scalar.  Values stay as they lie in memory and are
-// transposed by the LDS's transposing reads (a group of 16 lanes gets 4 keys of 16 dims, 4 keys a lane).  The 16-byte chunks of a row are
-// XOR-swizzled by the row, on the global side: 16 consecutive rows then offer one chunk in 16 places (the keys' 16-byte reads), and four consecutive
-// rows four neighbouring chunks in 4 different quarters of the banks (the values' transposing reads).
+// Four wavefronts of 32 rows; tiles of 64 keys and values, double buffered, filled by direct global -> LDS loads.  Each
+// wavefront fetches 16 rows of a tile: rows of one page, so its page is a scalar, loaded a tile ahead through the scalar cache (whose
+// loads are waited for apart from the tiles in flight).  Values stay as they lie in memory and are transposed by the LDS's
+// transposing reads (a group of 16 lanes gets 4 keys of 16 dims, 4 keys a lane).  The 16-byte chunks of a row are XOR-swizzled by
+// the row, on the global side: 16 consecutive rows then offer one chunk in 16 places (the keys' 16-byte reads), and four
+// consecutive rows four neighbouring chunks in 4 different quarters of the banks (the values' transposing reads).
+// FEAT 0: plain or capped scores, with or without a window; 1: bias by distance; 2: positions that are not the slots' numbers.
 template <int DH>
 struct TileCfg {
   static constexpr int KT = 64, ROWS = 128;
   static constexpr int CH = DH / 8;                               // 16-byte chunks of a row
   static constexpr int RPI = 64 / CH;                             // rows that one load instruction of a wavefront fills
-  static constexpr int NI = KT / RPI / 4;                         // load instructions of a wavefront, for K and for V
+  static constexpr int NI = 16 / RPI;                             // load instructions of a wavefront, for K and for V
   static constexpr int TILE = KT * DH;                            // elements
-  static constexpr size_t LDS_BYTES = 4ull * TILE * 2 + 2 * KT * 4;  // and the tiles' positions
+  static constexpr int POS = 2 * 2 * TILE;                      // the tiles' positions follow, then a word a wavefront
+  static constexpr size_t LDS_BYTES = POS * 2 + 2 * KT * 4 + 16;           // 33 and 65 KiB: four and two workgroups a compute unit
   // place of chunk c of row r: c ^ swz(r)
   static __device__ __forceinline__ int swz(int r) {
     if (DH == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
     return (((r >> 1) & 1) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
-  }
-};
-
-// 64 entries of a sequence's row of the page table in a wavefront's registers
-struct PageWindow {
-  const int32_t* row;
-  int last, n_pages, base, ids;
-  __device__ __forceinline__ PageWindow(const PagedArgs& p, int b, int col)
-      : row(p.table + (size_t)b * p.max_pages), last(p.max_pages - 1), n_pages(p.n_pages) { fill(col); }
-  __device__ __forceinline__ void fill(int col) {
-    base = col;
-    ids = row[min(col + (int)(threadIdx.x & 63), last)];
-  }
-  // before the columns first .. last (fewer than 64) are asked for: a load, and the wait for it, must not come between others
-  __device__ __forceinline__ void cover(int first, int last_col) {
-    if (last_col - base >= 64) fill(first);
-  }
-  // page of a column that all lanes ask for, -1 if it is none
-  __device__ __forceinline__ int at(int col) const {
-    const int p = __builtin_amdgcn_readlane(ids, col - base);
-    return (uint32_t)p < (uint32_t)n_pages ? p : -1;
   }
 };
 
@@ -585,14 +563,13 @@ __device__ __forceinline__ uint2 lds_read_transposed(const uint16_t* p) {
 }
 
 template <int DH, int FEAT>
-__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_paged_tile_kernel(AttnArgs a) {
   typedef TileCfg<DH> C;
   constexpr int NF = DH / 32, KS = DH / 16;
   extern __shared__ __attribute__((aligned(16))) uint16_t tile_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  // the heads of a row block on neighbouring workgroups: with a multiple of eight heads each XCD keeps its own in its L2
-  const int h = blockIdx.x % a.p.n_kv, piece = blockIdx.x / a.p.n_kv % a.n_split;
-  const int n_blk = gridDim.x / (a.n_split * a.p.n_kv);
+  // (Heads dealt so that all blocks of a sequence's head share one XCD's L2 are slower: 16 prompts of 1024 tokens, 12 heads, 68 us for 62.)
+  const int h = blockIdx.x % a.p.n_kv, piece = blockIdx.x / a.p.n_kv % a.n_split, n_blk = gridDim.x / (a.n_split * a.p.n_kv);
   const RowBlock rb = row_block<C::ROWS>(a, n_blk - 1 - blockIdx.x / a.p.n_kv / a.n_split);     // the last, longest blocks first
   if (rb.b < 0) return;
   const SeqRange s = seq_range(a.p, rb.b);
@@ -611,43 +588,61 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
   const int t_last = s.len - s.q + min((m0 + 31) / a.G, s.q - 1);
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)rb.b * slots : nullptr;
+  // keys below this slot are out of the window of some row of the wavefront
+  const int w_first = FEAT == 2 || a.window <= 0 ? INT32_MIN : t_last - a.window + 1;
+
+  const uint16_t* qp = (const uint16_t*)a.q + (size_t)row * a.ld_q + head * DH;
+  bf16x8_t fq[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) fq[ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16 + half * 8);
   float slope = 0.f;
   int t_pos = t_slot;
   if (FEAT) {
     if (a.slopes) slope = a.slopes[head] * kLog2e;
     if (FEAT == 2 && t_slot >= 0) t_pos = pos[t_slot];
   }
+  // Whether the piece has a page that is none: such tiles are masked key by key.  Each wavefront leaves its answer in LDS.
+  int* bad_words = reinterpret_cast<int*>(tile_lds + C::POS + 2 * C::KT * 2);
+  {
+    bool bad = false;
+    for (int col = (k_lo >> a.p.page_shift) + tid; col <= (k_hi - 1) >> a.p.page_shift; col += 256)
+      bad |= (uint32_t)a.p.table[(size_t)rb.b * a.p.max_pages + col] >= (uint32_t)a.p.n_pages;
+    const int any = __ballot(bad) != 0;
+    if (lane == 0) bad_words[wave] = any;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // written before the first tile's barrier
+  }
 
-  PageWindow pages(a.p, rb.b, k_lo >> a.p.page_shift);
+  scalar_i32* table = (scalar_i32*)(uintptr_t)(a.p.table + (size_t)rb.b * a.p.max_pages);
   const int page_mask = (1 << a.p.page_shift) - 1;
-  // this lane's row and chunk in a load instruction; the swizzle looks at rows modulo 16, so it differs between instructions
-  const int ld_row = lane / C::CH, ld_slot = lane % C::CH;
-  bool bad_next = false;                                          // whether the tile being loaded has a page that is none
-  auto load = [&](int kb, int buf) {
-    pages.cover(kb >> a.p.page_shift, (kb + C::KT - 1) >> a.p.page_shift);
-    bad_next = false;
-    for (int col = kb >> a.p.page_shift; col <= (min(kb + C::KT, s.len) - 1) >> a.p.page_shift; ++col)
-      bad_next |= pages.at(col) < 0;
-    if (FEAT == 2 && wave == 3)
-      __builtin_amdgcn_global_load_lds(LLMC_GPTR(pos + min(kb + lane, slots - 1)),
-                                       LLMC_LPTR(tile_lds + 4 * C::TILE + buf * 2 * C::KT), 4, 0, 0);
+  const int r0 = wave * 16;                                       // this wavefront's rows of a tile
+  int src_off[C::NI];                                             // this lane's chunk in each of its load instructions
 #pragma unroll
-    for (int j = 0; j < C::NI; ++j) {
-      const int r0 = (wave * C::NI + j) * C::RPI, key = kb + r0;
-      const int page = max(pages.at(key >> a.p.page_shift), 0);
-      const size_t at = ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & page_mask)) * DH;
-      const int off = ld_row * DH + (ld_slot ^ C::swz(r0 + ld_row)) * 8;
-      uint16_t* dst = tile_lds + buf * 2 * C::TILE + r0 * DH;
-      __builtin_amdgcn_global_load_lds(LLMC_GPTR((const uint16_t*)a.k + at + off), LLMC_LPTR(dst), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(LLMC_GPTR((const uint16_t*)a.v + at + off), LLMC_LPTR(dst + C::TILE), 16, 0, 0);
-    }
+  for (int j = 0; j < C::NI; ++j) {
+    const int r = j * C::RPI + lane / C::CH;
+    src_off[j] = r * DH + ((lane % C::CH) ^ C::swz(r)) * 8;
+  }
+  int page_next = 0;
+  auto ask_page = [&](int t) { page_next = table[min((k_lo + t * C::KT + r0) >> a.p.page_shift, a.p.max_pages - 1)]; };
+  auto load = [&](int t, int stage) {
+    const int key = k_lo + t * C::KT + r0;
+    const int page = (uint32_t)page_next < (uint32_t)a.p.n_pages ? page_next : 0;
+    const size_t at = ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & page_mask)) * DH;
+    uint16_t* dst = tile_lds + stage * 2 * C::TILE + r0 * DH;
+#pragma unroll
+    for (int j = 0; j < C::NI; ++j)
+      __builtin_amdgcn_global_load_lds(LLMC_GPTR((const uint16_t*)a.k + at + src_off[j]), LLMC_LPTR(dst + j * C::RPI * DH), 16, 0, 0);
+#pragma unroll
+    for (int j = 0; j < C::NI; ++j)
+      __builtin_amdgcn_global_load_lds(LLMC_GPTR((const uint16_t*)a.v + at + src_off[j]),
+                                       LLMC_LPTR(dst + C::TILE + j * C::RPI * DH), 16, 0, 0);
+    if (FEAT == 2)                                                // every wavefront the same 64 words
+      __builtin_amdgcn_global_load_lds(LLMC_GPTR(pos + min(k_lo + t * C::KT + lane, slots - 1)),
+                                       LLMC_LPTR(tile_lds + C::POS + stage * 2 * C::KT), 4, 0, 0);
   };
-  if (n_tiles > 0) load(k_lo, 0);
+  ask_page(0);
+  if (n_tiles > 0) load(0, 0);
+  ask_page(1);
 
-  const uint16_t* qp = (const uint16_t*)a.q + (size_t)row * a.ld_q + head * DH;
-  bf16x8_t fq[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) fq[ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16 + half * 8);
   f32x16_t o[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f)
@@ -656,18 +651,23 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
   float m_run = -INFINITY, l_run = 0.f;
   const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
   const bool exact_sum = a.lse != nullptr;
+  bool bad = false;
   // fragment places: keys' row lane % 32 (the swizzle looks at 16 rows), values' row (lane % 16) / 4 of a group of four keys
   const int k_row = lane & 31, k_swz = C::swz(k_row);
   const int v_row = half * 4 + ((lane & 15) >> 2), v_col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 
   for (int t = 0; t < n_tiles; ++t) {
-    const int buf = t & 1, kb = k_lo + t * C::KT;
-    const bool bad = bad_next;
+    const int kb = k_lo + t * C::KT, stage = t & 1;
     LLMC_WAIT_VM(0);
-    dma::barrier();                                               // this tile is there, and the other buffer's readers are done
-    if (t + 1 < n_tiles) load(kb + C::KT, buf ^ 1);
-    uint16_t* sk = tile_lds + buf * 2 * C::TILE;
+    dma::barrier();                                               // this tile is there, and the other buffer has no readers
+    if (t + 1 < n_tiles) {
+      load(t + 1, stage ^ 1);
+      ask_page(t + 2);
+    }
+    uint16_t* sk = tile_lds + stage * 2 * C::TILE;
     uint16_t* sv = sk + C::TILE;
+    const int* tile_pos = reinterpret_cast<const int*>(tile_lds + C::POS + stage * 2 * C::KT);
+    if (t == 0) bad = __builtin_amdgcn_readfirstlane(bad_words[0] | bad_words[1] | bad_words[2] | bad_words[3]) != 0;
     if (kb + C::KT > s.len || bad) {
       // what lies behind the sequence in its last page may be anything, and 0 * anything is not always 0
       const int r = tid >> 2, key = kb + r;
@@ -694,15 +694,26 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = sc[i >> 4][i & 15];
     const auto off = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
-    const int key0 = kb + half * 4;
-    if (FEAT) {
-      const int* tile_pos = reinterpret_cast<const int*>(tile_lds + 4 * C::TILE + buf * 2 * C::KT) + half * 4;
-      transform(a, x, [&](int i) { return FEAT == 2 ? tile_pos[off(i)] : key0 + off(i); }, slope, t_pos);
+    const int key0 = kb + half * 4, away0 = t_slot - key0;
+    if (FEAT == 2) {
+      bias_scores(a, x, [&](int i) { return t_pos - tile_pos[half * 4 + off(i)]; }, slope);
+    } else if (FEAT == 1) {
+      if (a.softcap > 0.f) cap_scores(a, x);
+      const float base = (float)away0;                            // distances below 2^24 are exact
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = fmaf(-slope, base - (float)off(i), fmaf(x[i], a.mul, a.add));
+    } else if (a.softcap > 0.f) {
+      cap_scores(a, x);
+    }
+    if (FEAT != 2 && kb < w_first) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (away0 - off(i) >= a.window) x[i] = -INFINITY;
     }
     if (kb + C::KT - 1 > t_first) {
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (key0 + off(i) > t_slot) x[i] = -INFINITY;
+        if (off(i) > away0) x[i] = -INFINITY;
     }
     if (bad) {
 #pragma unroll
@@ -715,33 +726,32 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void attention_paged_tile_ke
     uint32_t ma, mb_;
     butterfly_pair_u32<32>(__float_as_uint(mx), ma, mb_);
     mx = fmaxf(__uint_as_float(ma), __uint_as_float(mb_));
-    const float m_new = fmaxf(m_run, FEAT ? mx : mx * a.scale2);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    if (__any(m_new > m_run)) {
-      const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+    const float m_new = FEAT ? mx : fmaf(mx, a.mul, a.add);
+    if (__any(m_new > m_run + kSlack)) {
+      const float m_top = fmaxf(m_run, m_new), corr = m_top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_top);
+      m_run = m_top;
       l_run *= corr;
 #pragma unroll
       for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[f][r] *= corr;
     }
-    m_run = m_new;
-    // the scale (of scores that are not transformed) enters the exponent as one fma
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;         // a row that has seen no key so far
+    const float minus = a.add - m_use;
     uint32_t pk[2][8];
-    float l_exact = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(FEAT ? x[i] - m_use : fmaf(x[i], a.scale2, -m_use));
-      const float p1 = __builtin_amdgcn_exp2f(FEAT ? x[i + 1] - m_use : fmaf(x[i + 1], a.scale2, -m_use));
-      pk[i >> 4][(i & 15) >> 1] = f32x2_to_bf16x2(p0, p1);
-      x[i] = p0; x[i + 1] = p1;
+      x[i] = __builtin_amdgcn_exp2f(FEAT ? x[i] - m_use : fmaf(x[i], a.mul, minus));
+      x[i + 1] = __builtin_amdgcn_exp2f(FEAT ? x[i + 1] - m_use : fmaf(x[i + 1], a.mul, minus));
+      pk[i >> 4][(i & 15) >> 1] = f32x2_to_bf16x2(x[i], x[i + 1]);
     }
     // The sum is that of the rounded weights, two an instruction: the weights of the value product then add up to one.  Where
     // the cached tokens' weights are wanted too, which are not rounded, it is that of the weights as they are.
     if (exact_sum) {
+      float l_tile = 0.f;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) l_exact += x[i];
-      l_run += l_exact;
+      for (int i = 0; i < 32; ++i) l_tile += x[i];
+      l_run += l_tile;
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -849,14 +859,15 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
       float x[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[r] = sc[r];
-      if (FEAT) {
-        const int4 v = FEAT == 2 ? reinterpret_cast<const int4*>(pos)[min(key0, slots - 4) >> 2]
-                           : make_int4(key0, key0 + 1, key0 + 2, key0 + 3);
+      if (FEAT == 2) {
+        const int4 v = reinterpret_cast<const int4*>(pos)[min(key0, slots - 4) >> 2];
         const int key_pos[4] = {v.x, v.y, v.z, v.w};
-        transform(a, x, [&](int i) { return key_pos[i]; }, slope, t_pos);
+        bias_scores(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
+      } else if (FEAT == 1) {
+        bias_scores(a, x, [&](int i) { return t_slot - key0 - i; }, slope);
       } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] *= a.scale2;
+        for (int r = 0; r < 4; ++r) x[r] *= a.mul;
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -1018,6 +1029,15 @@ Layout ws_layout(const Plan& p, int n_rows, int H, int DH, int n_seqs, int n_kv,
   return l;
 }
 
+template <int DH, int FEAT>
+llmc_status_t launch_tile(const AttnArgs& a, unsigned grid, hipStream_t st) {
+  static std::atomic<bool> lds_set[64];
+  const auto kernel = attention_paged_tile_kernel<DH, FEAT>;
+  LLMC_TRY(ensure_dynamic_lds((const void*)kernel, TileCfg<DH>::LDS_BYTES, lds_set));
+  LLMC_KERNEL_GGL(kernel, dim3(grid), dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
+  return LLMC_OK;
+}
+
 template <typename T, int DH, int FEAT>
 llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* weight, hipStream_t st) {
   const unsigned grid = (unsigned)(p.blocks * a.p.n_kv * p.n_split);
@@ -1028,10 +1048,8 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
       const size_t lds = (size_t)4 * p.join_rows * (DH + 4 + 2) * 4;
       LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), lds, st, a);
     } else if constexpr (sizeof(T) == 2) {
-      static std::atomic<bool> lds_set[64];
-      const auto kernel = attention_paged_tile_kernel<DH, FEAT>;
-      LLMC_TRY(ensure_dynamic_lds((const void*)kernel, TileCfg<DH>::LDS_BYTES, lds_set));
-      LLMC_KERNEL_GGL(kernel, dim3(grid), dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
+      if (FEAT == 1 && !a.slopes) LLMC_TRY((launch_tile<DH, 0>(a, grid, st)));
+      else LLMC_TRY((launch_tile<DH, FEAT>(a, grid, st)));
     } else {
       LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), dim3(grid), dim3(256), 0, st, a);
     }
@@ -1090,8 +1108,13 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   a.p = paged_args(kv, bt);
   a.q = q; a.out = out; a.k = kv->d_k; a.v = kv->d_v; a.ld_q = ld_q; a.ld_out = ld_out;
   a.H = at->n_heads; a.G = at->n_heads / kv->n_kv_heads;
-  a.scale2 = at->scale * kLog2e; a.softcap = at->softcap;
-  if (at->softcap > 0.f) { a.cap_in = (float)(2.0 * 1.4426950408889634 * at->scale / at->softcap); a.cap_out = at->softcap * kLog2e; }
+  a.softcap = at->softcap;
+  a.mul = at->scale * kLog2e;
+  if (at->softcap > 0.f) {
+    a.cap_in = (float)(2.0 * 1.4426950408889634 * at->scale / at->softcap);
+    a.add = at->softcap * kLog2e;
+    a.mul = 2.f * a.add;
+  }
   a.window = at->window; a.slopes = at->d_slopes;
   a.pos = (at->window > 0 || at->d_slopes) ? bt->d_pos : nullptr;
   a.split = p.split; a.n_split = p.n_split;
