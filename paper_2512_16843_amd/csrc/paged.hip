@@ -58,10 +58,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // their number is at most the number of evicted tokens (closing the gaps in order would move nearly every token for each
 // one that goes).
 //
-// The choice: one workgroup per sequence narrows a 64-bit key (protected flag, weight, position) to the (n - k)-th smallest
-// by its digits of 8 bits, most significant first (a histogram in LDS a digit), then numbers holes and movers by a prefix
-// sum over the slots.
-constexpr int kSelThreads = 1024;
+// The choice: one workgroup per sequence.  A token's key is 64 bits (protected flag, weight, position); the (n - k)-th smallest is
+// narrowed by digits of 11 bits, most significant first, a histogram in LDS a digit, until at most 64 keys share the digits
+// so far (two digits, as weights go); a wavefront then ranks those by key and slot.  Holes and movers are numbered by counts
+// of ballots.  Up to 32768 tokens the keys are read once and stay in registers.  Bound: latency, one workgroup's chain of loads and
+// barriers.  SELECT_US
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kDigit = 11, kBins = 1 << kDigit;
 
 struct EvictArgs {
   const int32_t* table;
@@ -73,7 +75,7 @@ struct EvictArgs {
   int32_t sink, recent;
   int32_t* length_out;
   int32_t* counts;             // [n_seqs] number of moves
-  int2* moves;                 // [n_seqs, max_moves] (source slot, destination slot)
+  int4* moves;                 // [n_seqs, max_moves] source slot and page, destination slot and page
   int32_t max_moves;
 };
 
@@ -90,126 +92,241 @@ __device__ __forceinline__ uint64_t evict_key(float w, int pos, int last, int si
   return ((uint64_t)safe << 63) | ((uint64_t)weight_order(w) << 31) | p;
 }
 
+// E: tokens of a thread, kept in registers; 0: read again in every pass
+template <int E>
 __global__ __launch_bounds__(kSelThreads) void kv_evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t wave_sum_s[2][kSelThreads / 64];
-  __shared__ int sh_last;
-  __shared__ uint32_t sh_digit, sh_before;
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t totals[kSelWaves];
+  __shared__ uint32_t sh_digit, sh_before, sh_count, sh_n;
+  __shared__ int sh_last[kSelWaves], sh_slot;
+  __shared__ uint64_t sh_key;
+  __shared__ uint64_t cand_key[64];
+  __shared__ int cand_slot[64];
+  __shared__ uint32_t ballots[2][kSelWaves * (E ? E : 1)];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = min(max(a.length[b], 0), a.max_len);
   const int keep = min(max(a.keep[b], 0), n);
   const size_t slots = (size_t)a.max_pages << a.page_shift;
-  int32_t* pos = a.pos + b * slots;
-  float* weight = a.weight + b * slots;
-  if (tid == 0) a.length_out[b] = keep;
+  const int32_t* pos = a.pos + b * slots;
+  const float* weight = a.weight + b * slots;
   if (keep >= n) {
-    if (tid == 0) a.counts[b] = 0;
+    if (tid == 0) {
+      a.length_out[b] = keep;
+      a.counts[b] = 0;
+    }
     return;
   }
-  if (tid == 0) sh_last = INT32_MIN;
-  __syncthreads();
+  const int rounds = E ? E : (n + kSelThreads - 1) / kSelThreads;
+  uint64_t key[E ? E : 1];
   int last = INT32_MIN;
-  for (int j = tid; j < n; j += kSelThreads) last = max(last, pos[j]);
-  atomicMax(&sh_last, last);
+  if (E) {
+    float w[E ? E : 1];
+    int p[E ? E : 1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int j = min(e * kSelThreads + tid, n - 1);
+      w[e] = weight[j];
+      p[e] = pos[j];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) last = max(last, p[e]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) key[e] = ((uint64_t)__float_as_uint(w[e]) << 32) | (uint32_t)p[e];
+  } else {
+    for (int j = tid; j < n; j += kSelThreads) last = max(last, pos[j]);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) last = max(last, __shfl_xor(last, o, 64));
+  if (lane == 0) sh_last[wave] = last;
+  for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+  if (tid == 0) sh_n = 0;
   __syncthreads();
-  last = sh_last;
-  // the digits of the (n - keep)-th smallest key
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) last = max(last, sh_last[w]);
+  if (E) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      key[e] = evict_key(__uint_as_float((uint32_t)(key[e] >> 32)), (int)(uint32_t)key[e], last, a.sink, a.recent);
+  }
+  const auto key_at = [&](int e, int j) {
+    return E ? key[E ? e : 0] : evict_key(weight[j], pos[j], last, a.sink, a.recent);
+  };
+  // digits of the key, then (equal keys only) of the slot, until at most 64 tokens are left to choose among
   uint64_t prefix = 0;
-  uint32_t need = n - keep;            // still to be found among the keys that share the prefix
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += kSelThreads) {
-      const uint64_t key = evict_key(weight[j], pos[j], last, a.sink, a.recent);
-      if (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      uint32_t c[4], sum = 0;
+  uint32_t slot_prefix = 0, need = n - keep, count = n;
+  int shift = 64, slot_shift = 31;
+  while (count > 64) {
+    const bool by_slot = shift == 0;
+    const int to = by_slot ? max(slot_shift - kDigit, 0) : max(shift - kDigit, 0);
+    const uint32_t mask = (1u << ((by_slot ? slot_shift : shift) - to)) - 1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { c[i] = hist[lane * 4 + i]; sum += c[i]; }
-      uint32_t incl = sum;
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t v = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += v;
-      }
-      uint32_t before = incl - sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (before < need && need <= before + c[i]) { sh_digit = lane * 4 + i; sh_before = before; }
-        before += c[i];
+    for (int e = 0; e < rounds; ++e) {
+      const int j = e * kSelThreads + tid;
+      if (j < n) {
+        const uint64_t k = key_at(e, j);
+        if (by_slot) {
+          if (k == prefix && (slot_shift == 31 || ((uint32_t)j >> slot_shift) == (slot_prefix >> slot_shift)))
+            atomicAdd(&hist[((uint32_t)j >> to) & mask], 1u);
+        } else if (shift == 64 || (k >> shift) == (prefix >> shift)) {
+          atomicAdd(&hist[(uint32_t)(k >> to) & mask], 1u);
+        }
       }
     }
     __syncthreads();
-    prefix |= (uint64_t)sh_digit << shift;
+    const uint32_t c0 = hist[2 * tid], c1 = hist[2 * tid + 1];
+    uint32_t incl = c0 + c1;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t v = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 63) totals[wave] = incl;
+    hist[2 * tid] = 0;
+    hist[2 * tid + 1] = 0;
+    __syncthreads();
+    uint32_t before = incl - c0 - c1;
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) before += w < wave ? totals[w] : 0;
+    if (before < need && need <= before + c0) { sh_digit = 2 * tid; sh_before = before; sh_count = c0; }
+    before += c0;
+    if (before < need && need <= before + c1) { sh_digit = 2 * tid + 1; sh_before = before; sh_count = c1; }
+    __syncthreads();
+    if (by_slot) {
+      slot_prefix |= sh_digit << to;
+      slot_shift = to;
+    } else {
+      prefix |= (uint64_t)sh_digit << to;
+      shift = to;
+    }
     need -= sh_before;
-    __syncthreads();
+    count = sh_count;
+    if (by_slot && to == 0) break;                               // one token is left
   }
-  // `need` tokens whose key equals the prefix go too, those in the lowest slots (positions of one sequence differ, so it is one)
-  uint32_t eq_before = 0, hole_base = 0, mover_base = 0;
-  int2* moves = a.moves + (size_t)b * a.max_moves;
-  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const uint64_t key = j < n ? evict_key(weight[j], pos[j], last, a.sink, a.recent) : ~0ull;
-    const bool eq = j < n && key == prefix;
-    const uint64_t m_eq = __ballot(eq);
-    if (lane == 0) wave_sum_s[0][wave] = __popcll(m_eq);
-    __syncthreads();
-    uint32_t my_eq = eq_before, all_eq = 0;
-    for (int w = 0; w < kSelThreads / 64; ++w) {
-      if (w < wave) my_eq += wave_sum_s[0][w];
-      all_eq += wave_sum_s[0][w];
+#pragma unroll
+  for (int e = 0; e < rounds; ++e) {
+    const int j = e * kSelThreads + tid;
+    if (j >= n) continue;
+    const uint64_t k = key_at(e, j);
+    const bool in = shift == 64 || ((k >> shift) == (prefix >> shift) &&
+                                    (slot_shift == 31 || ((uint32_t)j >> slot_shift) == (slot_prefix >> slot_shift)));
+    if (in) {
+      const uint32_t at = atomicAdd(&sh_n, 1u);                   // at most 64; their order does not matter
+      if (at < 64) { cand_key[at] = k; cand_slot[at] = j; }
     }
-    eq_before += all_eq;
-    my_eq += __popcll(m_eq & ((1ull << lane) - 1));
-    __syncthreads();
-    const bool gone = j < n && (key < prefix || (eq && my_eq < need));
-    const bool hole = gone && j < keep, mover = j < n && !gone && j >= keep;
-    const uint64_t m_hole = __ballot(hole), m_move = __ballot(mover);
-    if (lane == 0) { wave_sum_s[0][wave] = __popcll(m_hole); wave_sum_s[1][wave] = __popcll(m_move); }
-    __syncthreads();
-    uint32_t my_hole = hole_base, my_move = mover_base;
-    for (int w = 0; w < kSelThreads / 64; ++w) {
-      const uint32_t ch = wave_sum_s[0][w], cm = wave_sum_s[1][w];
-      if (w < wave) { my_hole += ch; my_move += cm; }
-      hole_base += ch;
-      mover_base += cm;
-    }
-    my_hole += __popcll(m_hole & ((1ull << lane) - 1));
-    my_move += __popcll(m_move & ((1ull << lane) - 1));
-    if (hole && my_hole < (uint32_t)a.max_moves) moves[my_hole].y = j;
-    if (mover && my_move < (uint32_t)a.max_moves) moves[my_move].x = j;
-    __syncthreads();
   }
-  // as many holes as movers
-  const uint32_t n_moves = min(hole_base, (uint32_t)a.max_moves);
-  if (tid == 0) a.counts[b] = (int)n_moves;
-  __threadfence_block();
   __syncthreads();
-  for (uint32_t i = tid; i < n_moves; i += kSelThreads) {
-    const int2 m = moves[i];
-    pos[m.y] = pos[m.x];
-    weight[m.y] = weight[m.x];
+  if (wave == 0) {
+    const uint64_t mine = lane < (int)count ? cand_key[lane] : ~0ull;
+    const int my_slot = lane < (int)count ? cand_slot[lane] : INT32_MAX;
+    uint32_t rank = 0;
+    for (int i = 0; i < (int)count; ++i) rank += cand_key[i] < mine || (cand_key[i] == mine && cand_slot[i] < my_slot);
+    if (lane < (int)count && rank == need - 1) { sh_key = mine; sh_slot = my_slot; }
+  }
+  __syncthreads();
+  // gone: up to this key and, among equal keys, up to this slot
+  const uint64_t top = sh_key;
+  const int top_slot = sh_slot;
+  int4* moves = a.moves + (size_t)b * a.max_moves;
+  const int32_t* table = a.table + (size_t)b * a.max_pages;
+  const auto page = [&](int slot) {
+    const int p = table[slot >> a.page_shift];
+    return (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
+  };
+  // 0: stays where it is, 1: a hole, 2: moves
+  const auto part_of = [&](uint64_t k, int j) {
+    const bool gone = k < top || (k == top && j <= top_slot);
+    return j >= n ? 0 : gone ? (j < keep ? 1 : 0) : (j >= keep ? 2 : 0);
+  };
+  const auto put = [&](int part, int j, uint32_t hole_at, uint32_t move_at) {
+    if (part == 1 && hole_at < (uint32_t)a.max_moves) {
+      moves[hole_at].z = j;
+      moves[hole_at].w = page(j);
+    }
+    if (part == 2 && move_at < (uint32_t)a.max_moves) {
+      moves[move_at].x = j;
+      moves[move_at].y = page(j);
+    }
+  };
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t holes = 0;
+  if (E) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int j = e * kSelThreads + tid, part = part_of(key[E ? e : 0], j);
+      const uint64_t h = __ballot(part == 1), m = __ballot(part == 2);
+      if (lane == 0) {
+        ballots[0][e * kSelWaves + wave] = __popcll(h);
+        ballots[1][e * kSelWaves + wave] = __popcll(m);
+      }
+    }
+    __syncthreads();
+    if (wave < 2) {                                              // running sums in the tokens' order, in place
+      uint32_t base = 0;
+      for (int i0 = 0; i0 < E * kSelWaves; i0 += 64) {
+        const int i = i0 + lane;
+        const uint32_t c = i < E * kSelWaves ? ballots[wave][i] : 0;
+        uint32_t incl = c;
+        for (int o = 1; o < 64; o <<= 1) {
+          const uint32_t v = __shfl_up(incl, o, 64);
+          if (lane >= o) incl += v;
+        }
+        if (i < E * kSelWaves) ballots[wave][i] = base + incl - c;
+        base += __shfl(incl, 63, 64);
+      }
+      if (wave == 0 && lane == 0) sh_count = base;
+    }
+    __syncthreads();
+    holes = sh_count;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int j = e * kSelThreads + tid, part = part_of(key[E ? e : 0], j);
+      const uint64_t h = __ballot(part == 1), m = __ballot(part == 2);
+      put(part, j, ballots[0][e * kSelWaves + wave] + __popcll(h & below), ballots[1][e * kSelWaves + wave] + __popcll(m & below));
+    }
+  } else {
+    uint32_t movers = 0;
+    for (int e = 0; e < rounds; ++e) {
+      const int j = e * kSelThreads + tid, part = part_of(key_at(0, min(j, n - 1)), j);
+      const uint64_t h = __ballot(part == 1), m = __ballot(part == 2);
+      __syncthreads();
+      if (lane == 0) { totals[wave] = __popcll(h); ballots[1][wave] = __popcll(m); }
+      __syncthreads();
+      uint32_t my_hole = holes + __popcll(h & below), my_move = movers + __popcll(m & below);
+      for (int w = 0; w < kSelWaves; ++w) {
+        const uint32_t ch = totals[w], cm = ballots[1][w];
+        if (w < wave) { my_hole += ch; my_move += cm; }
+        holes += ch;
+        movers += cm;
+      }
+      put(part, j, my_hole, my_move);
+    }
+  }
+  if (tid == 0) {
+    a.length_out[b] = keep;
+    a.counts[b] = (int)min(holes, (uint32_t)a.max_moves);        // as many holes as movers
   }
 }
 
-// moves keys and values: 16 bytes a lane, the vectors of one head's token on neighbouring lanes; grid (pieces, n_seqs)
+// moves keys and values, 16 bytes a lane, the vectors of one head's token on neighbouring lanes, and positions and weights; grid
+// (pieces, n_seqs)
 __global__ __launch_bounds__(256) void kv_evict_move_kernel(EvictArgs a, uint4* __restrict__ k, uint4* __restrict__ v,
                                                             int vec_shift) {
   const int b = blockIdx.y;
   const int n_moves = a.counts[b];
-  const int2* moves = a.moves + (size_t)b * a.max_moves;
-  const int32_t* table = a.table + (size_t)b * a.max_pages;
+  const int4* moves = a.moves + (size_t)b * a.max_moves;
   const int mask = (1 << a.page_shift) - 1, per = a.n_kv << vec_shift;
   const int64_t total = (int64_t)n_moves * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int mv = (int)(i / per), r = (int)(i - (int64_t)mv * per);
     const int h = r >> vec_shift, c = r & ((1 << vec_shift) - 1);
-    const int2 m = moves[mv];
-    const int ps = table[m.x >> a.page_shift], pd = table[m.y >> a.page_shift];
-    if ((uint32_t)ps >= (uint32_t)a.n_pages || (uint32_t)pd >= (uint32_t)a.n_pages) continue;
-    const size_t src = (((((size_t)ps * a.n_kv + h) << a.page_shift) + (m.x & mask)) << vec_shift) + c;
-    const size_t dst = (((((size_t)pd * a.n_kv + h) << a.page_shift) + (m.y & mask)) << vec_shift) + c;
+    const int4 m = moves[mv];
+    if (r == 0) {
+      const size_t row = ((size_t)b * a.max_pages) << a.page_shift;
+      a.pos[row + m.z] = a.pos[row + m.x];
+      a.weight[row + m.z] = a.weight[row + m.x];
+    }
+    if (m.y < 0 || m.w < 0) continue;
+    const size_t src = (((((size_t)m.y * a.n_kv + h) << a.page_shift) + (m.x & mask)) << vec_shift) + c;
+    const size_t dst = (((((size_t)m.w * a.n_kv + h) << a.page_shift) + (m.z & mask)) << vec_shift) + c;
     const uint4 x = k[src], y = v[src];
     k[dst] = x;
     v[dst] = y;
@@ -247,7 +364,7 @@ llmc_status_t launch_kv_append(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* 
 
 // a sequence moves at most half of its tokens: as many as stay and as many as go
 size_t kv_evict_ws_bytes(int n_seqs, int max_len) {
-  return align_up((size_t)n_seqs * 4, 256) + (size_t)n_seqs * (max_len / 2 + 1) * sizeof(int2);
+  return align_up((size_t)n_seqs * 4, 256) + (size_t)n_seqs * (max_len / 2 + 1) * sizeof(int4);
 }
 
 llmc_status_t launch_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const int32_t* keep, int sink, int recent,
@@ -258,10 +375,14 @@ llmc_status_t launch_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* b
   a.page_shift = log2_of(kv->page_size); a.n_kv = kv->n_kv_heads;
   a.pos = bt->d_pos; a.weight = bt->d_weight; a.keep = keep; a.sink = sink; a.recent = recent; a.length_out = length_out;
   a.counts = (int32_t*)ws;
-  a.moves = (int2*)((char*)ws + align_up((size_t)bt->n_seqs * 4, 256));
+  a.moves = (int4*)((char*)ws + align_up((size_t)bt->n_seqs * 4, 256));
   a.max_moves = bt->max_len / 2 + 1;
   { ProfScope ps_("kv_evict_select_kernel", st);
-    LLMC_KERNEL_GGL(kv_evict_select_kernel, dim3((unsigned)bt->n_seqs), dim3(kSelThreads), 0, st, a); }
+    const dim3 grid((unsigned)bt->n_seqs), block(kSelThreads);
+    if (bt->max_len <= 2 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<2>, grid, block, 0, st, a);
+    else if (bt->max_len <= 8 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<8>, grid, block, 0, st, a);
+    else if (bt->max_len <= 32 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<32>, grid, block, 0, st, a);
+    else LLMC_KERNEL_GGL(kv_evict_select_kernel<0>, grid, block, 0, st, a); }
   LLMC_LAUNCH_CHECK("kv_evict_select");
   const int vec_shift = log2_of(kv->head_dim * (int)elem_size(kv->dtype) / 16);
   const int64_t most = (int64_t)a.max_moves * (kv->n_kv_heads << vec_shift);

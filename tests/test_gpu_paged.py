@@ -232,11 +232,14 @@ EVICT = [
     ([1500, 1500], [700, 701], 0, 2000),          # everything is protected
     ([3000], [1], 1, 0),
     ([64, 64], [-3, 0], 2, 2),
+    ([65, 128, 5000], [64, 64, 4999], 0, 0),
+    ([8192, 8193, 66], [2000, 8192, 1], 4, 100),
+    ([20000, 33000], [15000, 16000], 16, 64),
 ]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("kind", ["spread", "ties", "odd"])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd", "same"])
 @pytest.mark.parametrize("lens,keep,sink,recent", EVICT, ids=lambda x: "-".join(map(str, x)) if isinstance(x, list) else str(x))
 def test_evict(L, dtype, kind, lens, keep, sink, recent):
     kv, dh, page = 3, 64 if dtype == "bf16" else 128, 16
@@ -248,6 +251,9 @@ def test_evict(L, dtype, kind, lens, keep, sink, recent):
     weight = torch.exp(2 * torch.randn((B, slots), generator=g))
     if kind == "ties":
         weight = torch.randint(0, 3, (B, slots), generator=g).float()
+    if kind == "same":           # positions that repeat are not promised to be sensible, but the order is: by slot
+        weight.fill_(0.5)
+        pos //= 1000
     if kind == "odd":
         for x, every in ((float("nan"), 7), (float("inf"), 5), (-1.0, 3), (-0.0, 4), (0.0, 11)):
             weight[:, ::every] = x
