@@ -13,6 +13,7 @@
 #include <algorithm>
 #include "paged.h"
 #include "mma.h"
+#include "gemm.h"
 
 namespace llmc {
 namespace {
@@ -31,6 +32,7 @@ struct AttnArgs {
   const void *k, *v;
   int64_t ld_q, ld_out;
   int32_t H, G;
+  uint64_t g_magic, split_magic;   // row_magic of G and of split
   float softcap;
   float mul, add;              // a score in base 2 from a product (scale * log2(e), 0) or, capped, from y (2 c, c; c = softcap * log2(e))
   float cap_in;                // scale * 2 log2(e) / softcap
@@ -63,11 +65,17 @@ __device__ __forceinline__ float sum_over_groups(float v) {
   return __uint_as_float(a) + __uint_as_float(b);
 }
 
+// r / d by row_magic(d), r >= 0: a short launch runs through its code once, from a cold cache, and a division is thirty instructions
+__device__ __forceinline__ int div_by(int r, uint64_t magic) {
+  return (int)(((uint64_t)(uint32_t)r * (uint32_t)(magic >> 32) + __umulhi((uint32_t)r, (uint32_t)magic)) >> 29);
+}
+__device__ __forceinline__ int token_of(const AttnArgs& a, int m) { return a.G == 1 ? m : div_by(m, a.g_magic); }
+
 // the keys that rows [m0, m0 + rows) of a sequence's head can see: [lo, hi), lo a multiple of 64
 struct KeyRange { int lo, hi; };
 __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, const SeqRange& s, int m0, int rows) {
-  const int t0 = s.len - s.q + m0 / a.G;                                   // slot of the first row's token
-  const int t1 = s.len - s.q + min((m0 + rows - 1) / a.G, s.q - 1);
+  const int t0 = s.len - s.q + token_of(a, m0);                            // slot of the first row's token
+  const int t1 = s.len - s.q + min(token_of(a, m0 + rows - 1), s.q - 1);
   KeyRange r;
   r.hi = max(t1 + 1, 0);
   // positions rise by one at least from slot to slot unless tokens were moved, so a slot `window` away is out of the window
@@ -286,25 +294,24 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   constexpr int STEP = ROWSPLIT ? KEYS : NW * KEYS;
   extern __shared__ __attribute__((aligned(16))) float rows_lds[];          // ROWSPLIT 0: [NW][join_rows][LDO], then maxima, sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % a.p.n_kv, piece = blockIdx.x / a.p.n_kv % a.n_split;
-  const int unit = blockIdx.x / a.p.n_kv / a.n_split;
-  const RowBlock rb = ROWSPLIT ? row_block<ROWS>(a, unit, gridDim.x / (a.n_split * a.p.n_kv)) : RowBlock{a.by_length ? nth_longest(a.p, unit) : unit, 0};
+  const int h = blockIdx.x, piece = blockIdx.y, unit = blockIdx.z;
+  const RowBlock rb = ROWSPLIT ? row_block<ROWS>(a, unit, gridDim.z) : RowBlock{a.by_length ? nth_longest(a.p, unit) : unit, 0};
   if (rb.b < 0) return;
   const SeqRange s = seq_range(a.p, rb.b);
   const int rows = s.q * a.G;
   if (rb.mb * ROWS >= rows) return;
   const KeyRange kr = key_range(a, s, rb.mb * ROWS, ROWS);
-  const int n_pieces = max(1, (kr.hi - kr.lo + a.split - 1) / a.split);
+  const int n_pieces = max(1, div_by(kr.hi - kr.lo + a.split - 1, a.split_magic));
   if (piece >= n_pieces) return;
   const int k_lo = kr.lo + piece * a.split;
   int k_hi = min(kr.hi, k_lo + a.split);
   const int m0 = rb.mb * ROWS + (ROWSPLIT ? wave * 16 : 0);
   const int m = m0 + c;                                         // this lane's column
   const bool row_there = m < rows;
-  const int mc = min(m, rows - 1), i_new = mc / a.G, head = h * a.G + mc % a.G;
+  const int mc = min(m, rows - 1), i_new = token_of(a, mc), head = h * a.G + mc - i_new * a.G;
   const int row = s.first + i_new, t_slot = s.len - s.q + i_new;
-  const int t_first = s.len - s.q + m0 / a.G;                   // the first row's slot: all rows see the keys up to it
-  if (ROWSPLIT) k_hi = min(k_hi, max(0, s.len - s.q + min((m0 + 15) / a.G, s.q - 1) + 1));
+  const int t_first = s.len - s.q + token_of(a, m0);                   // the first row's slot: all rows see the keys up to it
+  if (ROWSPLIT) k_hi = min(k_hi, max(0, s.len - s.q + min(token_of(a, m0 + 15), s.q - 1) + 1));
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)rb.b * slots : nullptr;
   float slope = 0.f;
@@ -323,14 +330,16 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   // scores of these rows, for the weights that the keys receive
   float* score = a.scores && row_there ? a.scores + (((size_t)rb.b * a.p.n_kv + h) * a.join_rows + mc) * a.ld_scores + 4 * g : nullptr;
 
-  // A step's keys and values.  Pages are scalar loads, so waiting for them waits for no other load in flight; they are asked for one
-  // step earlier than the keys.  Beyond the last step the last one is read again (a conditional load would have to be waited for
-  // together with what is in flight).
+  // A step's keys and values.  The next step's keys are asked for as soon as the scores have consumed this one's, the values after
+  // the value product, into the same registers: one copy of the code (a second buffer, or a third, gains nothing where memory is
+  // the bound, and a longer code costs short calls).  Pages are scalar loads, so waiting for them waits for no other load in flight; they
+  // are asked for a step earlier than the keys.  Beyond the last step the last one is read again (a conditional load would have
+  // to be waited for together with what is in flight).
   struct Step {
     typename F::K k;
     typename F::V v;
     int4 pos[SUB];
-    int page[SUB];
+    int k_page[SUB], v_page[SUB];
   };
   scalar_i32* table = (scalar_i32*)(uintptr_t)(a.p.table + (size_t)rb.b * a.p.max_pages);
   const int k_first = k_lo + (ROWSPLIT ? 0 : wave * KEYS);
@@ -341,18 +350,33 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     for (int u = 0; u < SUB; ++u)
       page_next[u] = table[min((min(kb, k_last) + 16 * u) >> a.p.page_shift, a.p.max_pages - 1)];
   };
-  auto fetch = [&](Step& st, int kb) {
+  auto place = [&](int page, int key) {
+    return ((((size_t)max(page, 0) * a.p.n_kv + h) << a.p.page_shift) + (key & page_mask)) * DH;
+  };
+  auto fetch_k = [&](Step& st, int kb) {
     kb = min(kb, k_last);
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
-      st.page[u] = (uint32_t)page_next[u] < (uint32_t)a.p.n_pages ? page_next[u] : -1;
-      const size_t at = ((((size_t)max(st.page[u], 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
-      F::load_k(st.k, u, (const E*)a.k + at, c, g);
-      F::load_v(st.v, u, (const E*)a.v + at, c, g);
+      st.k_page[u] = (uint32_t)page_next[u] < (uint32_t)a.p.n_pages ? page_next[u] : -1;
+      F::load_k(st.k, u, (const E*)a.k + place(st.k_page[u], kb + 16 * u), c, g);
       if (FEAT == 2) st.pos[u] = reinterpret_cast<const int4*>(pos)[min(kb + 16 * u + 4 * g, slots - 4) >> 2];
     }
   };
-  auto work = [&](Step& st, int kb) {
+  auto fetch_v = [&](Step& st, int kb) {
+    kb = min(kb, k_last);
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      st.v_page[u] = st.k_page[u];
+      F::load_v(st.v, u, (const E*)a.v + place(st.v_page[u], kb + 16 * u), c, g);
+    }
+  };
+  if (k_first < k_hi) {
+    Step st;
+    ask_pages(k_first);
+    fetch_k(st, k_first);
+    fetch_v(st, k_first);
+    ask_pages(k_first + STEP);
+    for (int kb = k_first; kb < k_hi; kb += STEP) {
     float x[SUB * 4];
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
@@ -362,10 +386,17 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     }
     bool edge = kb + KEYS - 1 > t_first || kb + KEYS > s.len;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) edge |= st.page[u] < 0;
+    for (int u = 0; u < SUB; ++u) edge |= st.v_page[u] < 0;
+    int key_pos[8];
     if (FEAT == 2) {
-      const int key_pos[8] = {st.pos[0].x, st.pos[0].y, st.pos[0].z, st.pos[0].w, st.pos[SUB - 1].x, st.pos[SUB - 1].y,
-                              st.pos[SUB - 1].z, st.pos[SUB - 1].w};
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        key_pos[u * 4] = st.pos[u].x; key_pos[u * 4 + 1] = st.pos[u].y; key_pos[u * 4 + 2] = st.pos[u].z; key_pos[u * 4 + 3] = st.pos[u].w;
+      }
+    }
+    fetch_k(st, kb + STEP);
+    ask_pages(kb + 2 * STEP);
+    if (FEAT == 2) {
       bias_scores(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
     } else if (FEAT == 1) {
       const int away0 = t_slot - kb - 4 * g;
@@ -380,9 +411,9 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int key = kb + 16 * u + 4 * g + r;
-          if (key > t_slot || st.page[u] < 0) x[u * 4 + r] = -INFINITY;
+          if (key > t_slot || st.v_page[u] < 0) x[u * 4 + r] = -INFINITY;
           // what lies behind the sequence in its last page may be anything, and 0 * anything is not always 0
-          if (key >= s.len || st.page[u] < 0) F::clear_v(st.v, u, r);
+          if (key >= s.len || st.v_page[u] < 0) F::clear_v(st.v, u, r);
         }
     }
     if (!ROWSPLIT && score) {
@@ -412,23 +443,7 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
       l_run += pr[i >> 2][i & 3];
     }
     F::pv(st.v, pr, o);
-  };
-  if (k_first < k_hi) {
-    Step s0, s1;
-    ask_pages(k_first);
-    fetch(s0, k_first);
-    ask_pages(k_first + STEP);
-    for (int kb = k_first;;) {
-      fetch(s1, kb + STEP);
-      ask_pages(kb + 2 * STEP);
-      work(s0, kb);
-      kb += STEP;
-      if (kb >= k_hi) break;
-      fetch(s0, kb + STEP);
-      ask_pages(kb + 2 * STEP);
-      work(s1, kb);
-      kb += STEP;
-      if (kb >= k_hi) break;
+    fetch_v(st, kb + STEP);
     }
   }
   l_run = sum_over_groups(l_run);
@@ -487,7 +502,7 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
       l += f * sL[w * R + jr];
       y += f * rows_lds[(w * R + jr) * LDO + jd];
     }
-    const int jrow = s.first + jr / a.G, jhead = h * a.G + jr % a.G;
+    const int ji = token_of(a, jr), jrow = s.first + ji, jhead = h * a.G + jr - ji * a.G;
     const size_t rh = (size_t)jrow * a.H + jhead;
     if (n_pieces == 1) {
       Elem<T>::store((T*)a.out + (size_t)jrow * a.ld_out + jhead * DH + jd, y * (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l)));
@@ -542,7 +557,7 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   if (i >= s.q) return;
   const int m = i * a.G + head % a.G;
   const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
-  const int n = (kr.hi - kr.lo + a.split - 1) / a.split;
+  const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
   if (n > 1) join_pieces<T, DH>(a, row, head, n);               // else written where it was computed
 }
 
@@ -586,23 +601,23 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
   extern __shared__ __attribute__((aligned(16))) uint16_t tile_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   // (Heads dealt so that all blocks of a sequence's head share one XCD's L2 are slower: 16 prompts of 1024 tokens, 12 heads, 68 us for 62.)
-  const int h = blockIdx.x % a.p.n_kv, piece = blockIdx.x / a.p.n_kv % a.n_split, n_blk = gridDim.x / (a.n_split * a.p.n_kv);
-  const RowBlock rb = row_block<C::ROWS>(a, blockIdx.x / a.p.n_kv / a.n_split, n_blk);
+  const int h = blockIdx.x, piece = blockIdx.y;
+  const RowBlock rb = row_block<C::ROWS>(a, blockIdx.z, gridDim.z);
   if (rb.b < 0) return;
   const SeqRange s = seq_range(a.p, rb.b);
   const int rows = s.q * a.G;
   if (rb.mb * C::ROWS >= rows) return;
   const KeyRange kr = key_range(a, s, rb.mb * C::ROWS, C::ROWS);
-  const int n_pieces = max(1, (kr.hi - kr.lo + a.split - 1) / a.split);
+  const int n_pieces = max(1, div_by(kr.hi - kr.lo + a.split - 1, a.split_magic));
   if (piece >= n_pieces) return;
   const int k_lo = kr.lo + piece * a.split, k_hi = min(kr.hi, k_lo + a.split);
   const int n_tiles = (k_hi - k_lo + C::KT - 1) / C::KT;
   const int m0 = rb.mb * C::ROWS + wave * 32, m = m0 + (lane & 31);
   const bool row_there = m < rows;
-  const int mc = min(m, rows - 1), i_new = mc / a.G, head = h * a.G + mc % a.G;
+  const int mc = min(m, rows - 1), i_new = token_of(a, mc), head = h * a.G + mc - i_new * a.G;
   const int row = s.first + i_new, t_slot = s.len - s.q + i_new;
-  const int t_first = s.len - s.q + m0 / a.G;
-  const int t_last = s.len - s.q + min((m0 + 31) / a.G, s.q - 1);
+  const int t_first = s.len - s.q + token_of(a, m0);
+  const int t_last = s.len - s.q + min(token_of(a, m0 + 31), s.q - 1);
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)rb.b * slots : nullptr;
   // keys below this slot are out of the window of some row of the wavefront
@@ -830,8 +845,7 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
   typedef typename F::E E;
   constexpr int SUB = F::SUB, NK = 4 / SUB;                      // 4 sub-tiles of 16 keys
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int n_kb = (a.p.max_len + kWeightKeys - 1) / kWeightKeys;
-  const int blk = blockIdx.x % n_kb, h = blockIdx.x / n_kb % a.p.n_kv, b = blockIdx.x / n_kb / a.p.n_kv;
+  const int blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const SeqRange s = seq_range(a.p, b);
   const int kb = blk * kWeightKeys + wave * 64;
   if (kb >= s.len) return;
@@ -858,7 +872,7 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
   int m_hi = rows;
   if (a.window > 0 && !a.pos) m_hi = (int)min((int64_t)rows, max((int64_t)0, (int64_t)kb + 63 - t_base + a.window) * a.G);
   for (int m0 = m_lo & ~15; m0 < m_hi; m0 += 16) {
-    const int m = m0 + c, mc = min(m, rows - 1), i_new = mc / a.G, head = h * a.G + mc % a.G;
+    const int m = m0 + c, mc = min(m, rows - 1), i_new = token_of(a, mc), head = h * a.G + mc - i_new * a.G;
     const int row = s.first + i_new, t_slot = t_base + i_new;
     typename F::Q fq;
     F::load_q(fq, (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
@@ -938,10 +952,11 @@ __global__ __launch_bounds__(256) void attention_paged_score_weights_kernel(Attn
   const int rows = s.q * a.G, n = a.p.n_kv * rows;
   if (rows == 0) return;
   const KeyRange kr = key_range(a, s, 0, 16);                    // lo is a multiple of 64
-  const int n_pieces = (kr.hi - kr.lo + a.split - 1) / a.split;
+  const int n_pieces = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
   if ((int)blockIdx.x >= n_kb) {
     const int r = ((int)blockIdx.x - n_kb) * 4 + wave, h = r / rows, m = r - h * rows;
-    if (r < n && n_pieces > 1) join_pieces<T, DH>(a, s.first + m / a.G, h * a.G + m % a.G, n_pieces);
+    const int i = token_of(a, m);
+    if (r < n && n_pieces > 1) join_pieces<T, DH>(a, s.first + i, h * a.G + m - i * a.G, n_pieces);
     return;
   }
   const int key = blockIdx.x * 256 + lane * 4;
@@ -953,7 +968,8 @@ __global__ __launch_bounds__(256) void attention_paged_score_weights_kernel(Attn
   for (int r = r0; r < r1; ++r) {
     const int h = r / rows, m = r - h * rows;
     const float4 x = *reinterpret_cast<const float4*>(src + ((size_t)h * a.join_rows + m) * a.ld_scores);
-    const size_t rh = (size_t)(s.first + m / a.G) * a.H + h * a.G + m % a.G;
+    const int i_new = token_of(a, m);
+    const size_t rh = (size_t)(s.first + i_new) * a.H + h * a.G + m - i_new * a.G;
     float lse;
     if (n_pieces > 1) {
       const float2* ml = a.part_ml + rh * a.n_split;
@@ -1047,28 +1063,28 @@ Layout ws_layout(const Plan& p, int n_rows, int H, int DH, int n_seqs, int n_kv,
 }
 
 template <int DH, int FEAT>
-llmc_status_t launch_tile(const AttnArgs& a, unsigned grid, hipStream_t st) {
+llmc_status_t launch_tile(const AttnArgs& a, dim3 grid, hipStream_t st) {
   static std::atomic<bool> lds_set[64];
   const auto kernel = attention_paged_tile_kernel<DH, FEAT>;
   LLMC_TRY(ensure_dynamic_lds((const void*)kernel, TileCfg<DH>::LDS_BYTES, lds_set));
-  LLMC_KERNEL_GGL(kernel, dim3(grid), dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
+  LLMC_KERNEL_GGL(kernel, grid, dim3(256), TileCfg<DH>::LDS_BYTES, st, a);
   return LLMC_OK;
 }
 
 template <typename T, int DH, int FEAT>
 llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* weight, hipStream_t st) {
-  const unsigned grid = (unsigned)(p.blocks * a.p.n_kv * p.n_split);
+  const dim3 grid((unsigned)a.p.n_kv, (unsigned)p.n_split, (unsigned)p.blocks);
   {
     ProfScope ps_("attention_paged_kernel", st);
     if (!p.tile && !p.rowsplit) {
       // 16 rows of 128 dims take 33.8 KiB: no more than a kernel may have without asking
       const size_t lds = (size_t)4 * p.join_rows * (DH + 4 + 2) * 4;
-      LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), dim3(grid), dim3(256), lds, st, a);
+      LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), grid, dim3(256), lds, st, a);
     } else if constexpr (sizeof(T) == 2) {
       if (FEAT == 1 && !a.slopes) LLMC_TRY((launch_tile<DH, 0>(a, grid, st)));
       else LLMC_TRY((launch_tile<DH, FEAT>(a, grid, st)));
     } else {
-      LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), dim3(grid), dim3(256), 0, st, a);
+      LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), grid, dim3(256), 0, st, a);
     }
   }
   LLMC_LAUNCH_CHECK("attention_paged");
@@ -1089,7 +1105,7 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
   } else if (weight) {
     const int n_kb = (a.p.max_len + kWeightKeys - 1) / kWeightKeys;
     { ProfScope ps_("attention_paged_weight_kernel", st);
-      LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), dim3((unsigned)((int64_t)n_kb * a.p.n_kv * a.p.n_seqs)),
+      LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), dim3((unsigned)n_kb, (unsigned)a.p.n_kv, (unsigned)a.p.n_seqs),
                       dim3(256), 0, st, a, sums); }
     LLMC_LAUNCH_CHECK("attention_paged_weight");
     { ProfScope ps_("attention_paged_add_weights_kernel", st);
@@ -1111,7 +1127,7 @@ size_t attention_paged_ws_bytes(int dtype, int head_dim, int n_kv, int H, int n_
 bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
   const Plan p = make_plan(dtype, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len);
   const int64_t most = 0x7FFFFFFF;
-  return p.blocks * n_kv <= most / p.n_split && (int64_t)n_rows * H <= most &&
+  return p.blocks <= 65535 && p.n_split <= 65535 && (int64_t)n_rows * H <= most && p.blocks * n_kv <= most / p.n_split &&
          (!weights || (int64_t)((max_len + kWeightKeys - 1) / kWeightKeys) * n_kv <= most / n_seqs);
 }
 
@@ -1125,6 +1141,7 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   a.p = paged_args(kv, bt);
   a.q = q; a.out = out; a.k = kv->d_k; a.v = kv->d_v; a.ld_q = ld_q; a.ld_out = ld_out;
   a.H = at->n_heads; a.G = at->n_heads / kv->n_kv_heads;
+  a.g_magic = row_magic(a.G); a.split_magic = row_magic(p.split);
   a.softcap = at->softcap;
   a.mul = at->scale * kLog2e;
   if (at->softcap > 0.f) {
