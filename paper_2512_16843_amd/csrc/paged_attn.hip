@@ -266,7 +266,8 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int blk, int n_
 }
 
 // The n-th sequence when each group of 64 is ordered by length, longest first.  In the order of the batch, lengths may repeat with the period
-// in which workgroups come back to a compute unit (64 sequences of up to 2048 tokens, 12 heads: 50 us, 42 in order).
+// in which workgroups come back to a compute unit (64 sequences of up to 2048 tokens, 12 heads: 50 us, 42 in order).  Pieces of a
+// long axis are better mixed (6 sequences of up to 32768, 8 heads of 128: 91 us, 100 in order).
 __device__ __forceinline__ int nth_longest(const PagedArgs& p, int n) {
   const int lane = threadIdx.x & 63, first = n & ~63;
   const int len = first + lane < p.n_seqs ? p.length[first + lane] : -1;
@@ -526,22 +527,28 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, int row, int head
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const float top_use = top == -INFINITY ? 0.f : top;
-  constexpr int PER = DH / 64;
-  float l = 0.f, y[PER];
-#pragma unroll
-  for (int t = 0; t < PER; ++t) y[t] = 0.f;
-#pragma unroll 8
-  for (int j = 0; j < n; ++j) {
+  // 16 bytes a lane: the wavefront takes 256 / DH pieces a step
+  constexpr int L = DH / 4, STEP = 64 / L;
+  const int sub = lane / L, dim = lane % L * 4;
+  float l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int j = sub; j < n; j += STEP) {
     const float2 v = ml[j];
+    const float4 p = *reinterpret_cast<const float4*>(po + (size_t)j * DH + dim);
     const float f = __builtin_amdgcn_exp2f(v.x - top_use);
     l += f * v.y;
+    y[0] += f * p.x; y[1] += f * p.y; y[2] += f * p.z; y[3] += f * p.w;
+  }
 #pragma unroll
-    for (int t = 0; t < PER; ++t) y[t] += f * po[(size_t)j * DH + t * 64 + lane];
+  for (int o = 32; o >= L; o >>= 1) {
+    l += __shfl_xor(l, o, 64);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] += __shfl_xor(y[t], o, 64);
   }
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
 #pragma unroll
-  for (int t = 0; t < PER; ++t)
-    Elem<T>::store((T*)a.out + (size_t)row * a.ld_out + head * DH + t * 64 + lane, y[t] * inv);
+  for (int t = 0; t < 4; ++t) y[t] *= inv;
+  if (sub == 0) store_vec<T, 4>((T*)a.out + (size_t)row * a.ld_out + head * DH + dim, y);
   if (a.lse && lane == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
 }
 
@@ -1157,7 +1164,7 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   a.lse = weights ? (float*)(w + l.lse) : nullptr;
   const int64_t levels = ((int64_t)bt->max_new * a.G + p.rows - 1) / p.rows;
   a.by_level = bt->n_seqs <= 64 && levels <= 64 ? (int)levels : 0;
-  a.by_length = bt->n_seqs > 1 && p.blocks * kv->n_kv_heads * p.n_split > 256;
+  a.by_length = bt->n_seqs > 1 && p.n_split == 1 && p.blocks * kv->n_kv_heads > 256;
   a.join_rows = p.join_rows; a.ld_scores = l.ld_scores;
   a.scores = weights && !p.tile && !p.rowsplit ? (float*)(w + l.scores) : nullptr;
   float* sums = weights ? (float*)(w + l.sums) : nullptr;
