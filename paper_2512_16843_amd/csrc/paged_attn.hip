@@ -972,33 +972,42 @@ __global__ __launch_bounds__(256) void attention_paged_score_weights_kernel(Attn
   const int per = (n + 3) / 4, r0 = wave * per, r1 = min(n, r0 + per);
   const float* src = a.scores + (size_t)b * a.p.n_kv * a.join_rows * a.ld_scores + (there ? key : kr.lo);
   float w[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int r = r0; r < r1; ++r) {
-    const int h = r / rows, m = r - h * rows;
-    const float4 x = *reinterpret_cast<const float4*>(src + ((size_t)h * a.join_rows + m) * a.ld_scores);
-    const int i_new = token_of(a, m);
+  for (int q0 = r0; q0 < r1; q0 += 8) {
+    // eight rows' normalisers side by side, by eight lanes each
+    const int r = min(q0 + (lane >> 3), r1 - 1), h = r / rows, m = r - h * rows, i_new = token_of(a, m);
+    const int at = h * a.join_rows + m;
     const size_t rh = (size_t)(s.first + i_new) * a.H + h * a.G + m - i_new * a.G;
     float lse;
     if (n_pieces > 1) {
       const float2* ml = a.part_ml + rh * a.n_split;
       float top = -INFINITY, l = 0.f;
-      for (int j = lane; j < n_pieces; j += 64) {
-        const float2 v = ml[j];
-        const float t = fmaxf(top, v.x), t_use = t == -INFINITY ? 0.f : t;
-        l = l * __builtin_amdgcn_exp2f(top - t_use) + v.y * __builtin_amdgcn_exp2f(v.x - t_use);
-        top = t;
-      }
-      float all = top;
+      for (int j = lane & 7; j < n_pieces; j += 8) top = fmaxf(top, ml[j].x);
 #pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-      const float all_use = all == -INFINITY ? 0.f : all;
-      l = wave_sum(l * __builtin_amdgcn_exp2f(top - all_use));
-      lse = l == 0.f ? INFINITY : all + __builtin_amdgcn_logf(l);
+      for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+      const float top_use = top == -INFINITY ? 0.f : top;
+      for (int j = lane & 7; j < n_pieces; j += 8) {
+        const float2 v = ml[j];
+        l += v.y * __builtin_amdgcn_exp2f(v.x - top_use);
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) l += __shfl_xor(l, o, 64);
+      lse = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
     } else {
       lse = a.lse[rh];
     }
-    const float xs[4] = {x.x, x.y, x.z, x.w};
+    float4 x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] += xs[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(xs[i] - lse);
+    for (int i = 0; i < 8; ++i)
+      x[i] = *reinterpret_cast<const float4*>(src + (size_t)__builtin_amdgcn_readlane(at, i * 8) * a.ld_scores);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (q0 + i >= r1) break;
+      const float z = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), i * 8));
+      w[0] += x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[i].x - z);
+      w[1] += x[i].y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[i].y - z);
+      w[2] += x[i].z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[i].z - z);
+      w[3] += x[i].w == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[i].w - z);
+    }
   }
   if (wave > 0) part[wave - 1][lane] = make_float4(w[0], w[1], w[2], w[3]);
   __syncthreads();
