@@ -841,79 +841,132 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
 }
 
 // ---- the weight that every key received ---------------------------------------------------------------------------------
-// sum over the rows of p = 2^(x - lse), the scores computed a second time with the finished normalisers.  A wavefront holds
-// 64 keys of one head in registers and walks the rows; its sums are per head (sums[b][h][key]), added up over the heads in
-// ascending order by the second kernel: no atomics, one order.
-constexpr int kWeightKeys = 256;                                 // a workgroup
+// sum over the rows of p = 2^(x - lse), the scores computed a second time with the finished normalisers.  A wavefront, a workgroup
+// of its own, holds 16 to 64 keys of one head in registers and walks the rows, the next ones in flight; where there are few, several share a
+// head's rows.  Its sums go to sums[b][share][h][key]; a second kernel adds them up in one order: no atomics.  The first keys, which
+// every row sees, come first.  (Workgroups that take all heads of some keys and add in LDS spare that launch, 4.6 us, but
+// are few and uneven: 16 prompts of 1024 tokens, 12 heads: 71 us, 54 this way.)
+// FEAT as in the tile kernel.
+template <typename T, int DH> struct WeightCfg {
+  static constexpr int TILES = sizeof(T) == 2 ? 4 : DH == 64 ? 2 : 1;        // of 16 keys: 32 or 64 registers
+  static constexpr int RT = sizeof(T) == 2 && DH == 64 ? 2 : 1;              // 16-row tiles of a step
+  static constexpr int KEYS = 16 * TILES;
+};
 
 template <typename T, int DH, int FEAT>
-__global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a, float* __restrict__ sums) {
+__global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, float* __restrict__ sums) {
   typedef Frag<T, DH> F;
   typedef typename F::E E;
-  constexpr int SUB = F::SUB, NK = 4 / SUB;                      // 4 sub-tiles of 16 keys
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  typedef WeightCfg<T, DH> W;
+  constexpr int SUB = F::SUB, TILES = W::TILES, NK = TILES / SUB, RT = W::RT;
+  const int lane = threadIdx.x, c = lane & 15, g = lane >> 4;
+  const int h = blockIdx.y, share = blockIdx.z, shares = gridDim.z;
+  const int b = blockIdx.x % a.p.n_seqs, kb = blockIdx.x / a.p.n_seqs * W::KEYS;
   const SeqRange s = seq_range(a.p, b);
-  const int kb = blk * kWeightKeys + wave * 64;
-  if (kb >= s.len) return;
+  if (kb >= s.len || s.q == 0) return;
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)b * slots : nullptr;
+  const int rows = s.q * a.G, t_base = s.len - s.q;
+  scalar_i32* table = (scalar_i32*)(uintptr_t)(a.p.table + (size_t)b * a.p.max_pages);
   const int page_mask = (1 << a.p.page_shift) - 1;
+  int page[TILES];
+  bool bad = false;
   typename F::K fk[NK];
-  bool no_page[4];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int page = page_of(a.p, b, kb + 16 * u);
-    no_page[u] = page < 0;
-    const size_t at = ((((size_t)max(page, 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
+  for (int u = 0; u < TILES; ++u) {
+    const int p = table[min((kb + 16 * u) >> a.p.page_shift, a.p.max_pages - 1)];
+    page[u] = (uint32_t)p < (uint32_t)a.p.n_pages ? p : -1;
+    bad |= page[u] < 0;
+    const size_t at = ((((size_t)max(page[u], 0) * a.p.n_kv + h) << a.p.page_shift) + ((kb + 16 * u) & page_mask)) * DH;
     F::load_k(fk[u / SUB], u % SUB, (const E*)a.k + at, c, g);
   }
-  float w[4][4];
+  int key_pos[TILES][4];
+  if (FEAT == 2) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) w[u][r] = 0.f;
-  const int rows = s.q * a.G, t_base = s.len - s.q;
+    for (int u = 0; u < TILES; ++u) {
+      const int4 v = reinterpret_cast<const int4*>(pos)[min(kb + 16 * u + 4 * g, slots - 4) >> 2];
+      key_pos[u][0] = v.x; key_pos[u][1] = v.y; key_pos[u][2] = v.z; key_pos[u][3] = v.w;
+    }
+  }
   // rows whose tokens do not lie before the first key, and, with a window and slots as positions, not too far behind the last
   const int m_lo = max(0, kb - t_base) * a.G;
   int m_hi = rows;
-  if (a.window > 0 && !a.pos) m_hi = (int)min((int64_t)rows, max((int64_t)0, (int64_t)kb + 63 - t_base + a.window) * a.G);
-  for (int m0 = m_lo & ~15; m0 < m_hi; m0 += 16) {
-    const int m = m0 + c, mc = min(m, rows - 1), i_new = token_of(a, mc), head = h * a.G + mc - i_new * a.G;
-    const int row = s.first + i_new, t_slot = t_base + i_new;
-    typename F::Q fq;
-    F::load_q(fq, (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
-    const float lse = m < rows ? a.lse[(size_t)row * a.H + head] : INFINITY;
-    float slope = 0.f;
-    int t_pos = t_slot;
-    if (FEAT) {
-      if (a.slopes) slope = a.slopes[head] * kLog2e;
-      if (FEAT == 2 && t_slot >= 0) t_pos = pos[t_slot];
+  if (FEAT != 2 && a.window > 0)
+    m_hi = (int)min((int64_t)rows, max((int64_t)0, (int64_t)kb + W::KEYS - 1 - t_base + a.window) * a.G);
+  struct Rows {
+    typename F::Q q[RT];
+    float lse[RT], slope[RT];
+    int t_slot[RT], t_pos[RT];
+  };
+  float w[TILES][4];
+#pragma unroll
+  for (int u = 0; u < TILES; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w[u][r] = 0.f;
+  auto fetch = [&](Rows& R, int m0) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int m = m0 + 16 * i + c, mc = min(m, rows - 1), i_new = token_of(a, mc), head = h * a.G + mc - i_new * a.G;
+      const int row = s.first + i_new;
+      F::load_q(R.q[i], (const E*)a.q + (size_t)row * a.ld_q + head * DH, g);
+      R.lse[i] = a.lse[(size_t)row * a.H + head];
+      R.t_slot[i] = t_base + i_new;
+      if (FEAT) R.slope[i] = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+      if (FEAT == 2) R.t_pos[i] = pos[max(R.t_slot[i], 0)];
     }
+  };
+  auto work = [&](Rows& R, int m0) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const f32x4_t sc = F::qk(fk[u / SUB], u % SUB, fq);
-      const int key0 = kb + 16 * u + 4 * g;
-      float x[4];
+    for (int i = 0; i < RT; ++i) {
+      const int first = t_base + token_of(a, min(m0 + 16 * i, rows - 1)), last = t_base + token_of(a, min(m0 + 16 * i + 15, rows - 1));
+      const bool edge = first < kb + W::KEYS - 1 || bad || (FEAT != 2 && a.window > 0 && (int64_t)last - kb >= a.window);
+      const float lse = m0 + 16 * i + c < m_hi ? R.lse[i] : INFINITY;       // no such row, or out of the window: weights of zero
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = sc[r];
-      if (FEAT == 2) {
-        const int4 v = reinterpret_cast<const int4*>(pos)[min(key0, slots - 4) >> 2];
-        const int key_pos[4] = {v.x, v.y, v.z, v.w};
-        bias_scores(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
-      } else if (FEAT == 1) {
-        bias_scores(a, x, [&](int i) { return t_slot - key0 - i; }, slope);
-      } else {
+      for (int u = 0; u < TILES; ++u) {
+        const f32x4_t sc = F::qk(fk[u / SUB], u % SUB, R.q[i]);
+        const int key0 = kb + 16 * u + 4 * g;
+        float x[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] *= a.mul;
+        for (int r = 0; r < 4; ++r) x[r] = sc[r];
+        if (FEAT == 2) {
+          bias_scores(a, x, [&](int r) { return R.t_pos[i] - key_pos[u][r]; }, R.slope[i]);
+        } else {
+          if (a.softcap > 0.f) cap_scores(a, x);
+          if (FEAT == 1) {
+            const float base = (float)(R.t_slot[i] - key0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = fmaf(-R.slope[i], base - (float)r, fmaf(x[r], a.mul, a.add));
+          }
+        }
+        if (edge) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int away = R.t_slot[i] - key0 - r;
+            if (away < 0 || page[u] < 0 || (FEAT != 2 && a.window > 0 && away >= a.window)) x[r] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          w[u][r] += __builtin_amdgcn_exp2f(FEAT ? x[r] - lse : fmaf(x[r], a.mul, a.add - lse));
       }
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        w[u][r] += key0 + r <= t_slot && !no_page[u] && lse < INFINITY ? __builtin_amdgcn_exp2f(x[r] - lse) : 0.f;
+    }
+  };
+  const int step = shares * RT * 16;
+  int m0 = (m_lo & ~15) + share * RT * 16;
+  if (m0 < m_hi) {
+    Rows r0, r1;
+    fetch(r0, m0);
+    for (;;) {
+      fetch(r1, m0 + step);                                      // beyond the last row the last one is read again
+      work(r0, m0);
+      if ((m0 += step) >= m_hi) break;
+      fetch(r0, m0 + step);
+      work(r1, m0);
+      if ((m0 += step) >= m_hi) break;
     }
   }
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
+  for (int u = 0; u < TILES; ++u)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float v = w[u][r];
@@ -923,26 +976,22 @@ __global__ __launch_bounds__(256) void attention_paged_weight_kernel(AttnArgs a,
       v += __uint_as_float(butterfly_u32<1>(__float_as_uint(v)));
       w[u][r] = v;
     }
-  if (c == 0) {
-    float* dst = sums + ((size_t)b * a.p.n_kv + h) * a.p.max_len;
+  if (c == 0) {                                                  // a row of sums has room for whole tiles
+    float* dst = sums + (((size_t)b * shares + share) * a.p.n_kv + h) * a.ld_scores + kb + 4 * g;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int key = kb + 16 * u + 4 * g + r;
-        if (key < s.len) dst[key] = w[u][r];
-      }
+    for (int u = 0; u < TILES; ++u) *reinterpret_cast<float4*>(dst + 16 * u) = make_float4(w[u][0], w[u][1], w[u][2], w[u][3]);
   }
 }
 
-__global__ __launch_bounds__(256) void attention_paged_add_weights_kernel(PagedArgs p, const float* __restrict__ sums,
-                                                                          float* __restrict__ weight) {
+__global__ __launch_bounds__(256) void attention_paged_add_weights_kernel(PagedArgs p, const float* __restrict__ sums, int n,
+                                                                          int ld, float* __restrict__ weight) {
   const int b = blockIdx.y, key = blockIdx.x * 256 + threadIdx.x;
   const SeqRange s = seq_range(p, b);
   if (key >= s.len || s.q == 0) return;
-  const float* src = sums + (size_t)b * p.n_kv * p.max_len + key;
+  const float* src = sums + (size_t)b * n * ld + key;
   float v = 0.f;
-  for (int h = 0; h < p.n_kv; ++h) v += src[(size_t)h * p.max_len];
+#pragma unroll 8
+  for (int h = 0; h < n; ++h) v += src[(size_t)h * ld];
   weight[((size_t)b * p.max_pages << p.page_shift) + key] += v;
 }
 
@@ -1030,6 +1079,7 @@ struct Plan {
   int join_rows;               // rows a head at most, where a workgroup's wavefronts are joined
   int64_t blocks;              // row blocks of all sequences, at most
   int split, n_split;
+  int shares;                  // of a head's rows, for the weights of its keys
 };
 
 // How a call is cut.  Up to 16 rows a head (single tokens above all): 16-row products with the keys dealt to wavefronts.  More
@@ -1058,6 +1108,10 @@ Plan make_plan(int dtype, int n_rows, int n_seqs, int n_kv, int G, int max_new, 
   want = std::max<int64_t>(1, want);
   p.split = (int)std::max<int64_t>(256, align_up((size_t)((max_len + want - 1) / want), 128));
   p.n_split = std::max(1, (int)((max_len + p.split - 1) / p.split));
+  // Wavefronts that sum weights: two a SIMD at least as long as each has 128 rows, and none with many more than 256 rows: the first keys
+  // of a long chunk would keep the call waiting (16 prompts of 1024 tokens, 12 heads: 64 us in one share, 54 in four).
+  const int64_t waves = (int64_t)n_seqs * n_kv * ((max_len + 63) / 64);
+  p.shares = (int)std::max<int64_t>(1, std::min<int64_t>({std::max<int64_t>(2048 / waves, rows / 256), rows / 128, 16}));
   return p;
 }
 
@@ -1068,12 +1122,12 @@ Layout ws_layout(const Plan& p, int n_rows, int H, int DH, int n_seqs, int n_kv,
   auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes, 256); return r; };
   const size_t rh = (size_t)n_rows * H;
   const bool scores = weights && !p.tile && !p.rowsplit;
-  l.ld_scores = (int)align_up((size_t)max_len, 16);
+  l.ld_scores = (int)align_up((size_t)max_len, 64);
   l.part_o = take(p.n_split > 1 ? rh * p.n_split * DH * 4 : 0);
   l.part_ml = take(p.n_split > 1 ? rh * p.n_split * 8 : 0);
   l.lse = take(weights ? rh * 4 : 0);
   l.scores = take(scores ? (size_t)n_seqs * n_kv * p.join_rows * l.ld_scores * 4 : 0);
-  l.sums = take(weights && !scores ? (size_t)n_seqs * n_kv * max_len * 4 : 0);
+  l.sums = take(weights && !scores ? (size_t)n_seqs * n_kv * p.shares * l.ld_scores * 4 : 0);
   l.total = std::max<size_t>(at, 256);
   return l;
 }
@@ -1119,14 +1173,15 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
                       n_kb); }
     LLMC_LAUNCH_CHECK("attention_paged_score_weights");
   } else if (weight) {
-    const int n_kb = (a.p.max_len + kWeightKeys - 1) / kWeightKeys;
+    constexpr int keys = WeightCfg<T, DH>::KEYS;
     { ProfScope ps_("attention_paged_weight_kernel", st);
-      LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), dim3((unsigned)n_kb, (unsigned)a.p.n_kv, (unsigned)a.p.n_seqs),
-                      dim3(256), 0, st, a, sums); }
+      const dim3 wg((unsigned)((a.p.max_len + keys - 1) / keys * a.p.n_seqs), (unsigned)a.p.n_kv, (unsigned)p.shares);
+      if (FEAT == 1 && !a.slopes) LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, 0>), wg, dim3(64), 0, st, a, sums);
+      else LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), wg, dim3(64), 0, st, a, sums); }
     LLMC_LAUNCH_CHECK("attention_paged_weight");
     { ProfScope ps_("attention_paged_add_weights_kernel", st);
       LLMC_KERNEL_GGL(attention_paged_add_weights_kernel, dim3((a.p.max_len + 255) / 256, a.p.n_seqs), dim3(256), 0, st, a.p,
-                      sums, weight); }
+                      sums, a.p.n_kv * p.shares, a.ld_scores, weight); }
     LLMC_LAUNCH_CHECK("attention_paged_add_weights");
   }
   return LLMC_OK;
@@ -1144,7 +1199,7 @@ bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs,
   const Plan p = make_plan(dtype, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len);
   const int64_t most = 0x7FFFFFFF;
   return p.blocks <= 65535 && p.n_split <= 65535 && (int64_t)n_rows * H <= most && p.blocks * n_kv <= most / p.n_split &&
-         (!weights || (int64_t)((max_len + kWeightKeys - 1) / kWeightKeys) * n_kv <= most / n_seqs);
+         (!weights || (int64_t)((max_len + 15) / 16) <= most / n_seqs);
 }
 
 llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at,
