@@ -477,8 +477,8 @@ static llmc_status_t check_attn(const llmc_kv_desc_t* kv, const llmc_kv_batch_t*
   REQUIRE(at->n_heads <= 65535 && (int64_t)bt->max_new * at->n_heads <= 0x7FFFFFFF, LLMC_ERR_SHAPE, "n_heads=%d is too large",
           at->n_heads);
   REQUIRE(at->accumulate == 0 || at->accumulate == 1, LLMC_ERR_INVALID_ARG, "accumulate must be 0 or 1");
-  REQUIRE(attention_paged_grid_ok(kv->dtype, kv->n_kv_heads, at->n_heads, bt->n_rows, bt->n_seqs, bt->max_new, bt->max_len,
-                                  at->accumulate == 1), LLMC_ERR_SHAPE, "the batch is too large for one launch");
+  REQUIRE(attention_paged_grid_ok(kv->dtype, kv->head_dim, kv->n_kv_heads, at->n_heads, bt->n_rows, bt->n_seqs, bt->max_new,
+                                  bt->max_len, at->accumulate == 1), LLMC_ERR_SHAPE, "the batch is too large for one launch");
   return LLMC_OK;
 }
 static llmc_status_t check_attn_values(const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at) {

@@ -384,7 +384,8 @@ llmc_status_t launch_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* b
 size_t attention_paged_ws_bytes(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len,
                                 bool weights);
 // whether the launches' sizes fit a grid
-bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights);
+bool attention_paged_grid_ok(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len,
+                             bool weights);
 llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at,
                                      const void* q, int64_t ld_q, void* out, int64_t ld_out, void* ws, hipStream_t st);
 // the decoder block on new tokens (bt->n_rows of them)

@@ -552,7 +552,8 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, int row, int head
   if (a.lse && lane == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
 }
 
-template <typename T, int DH, int ROWS>
+// one token of each sequence, or few: a wavefront a (row, head)
+template <typename T, int DH>
 __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (rh >= (int64_t)a.p.n_rows * a.H) return;
@@ -560,12 +561,49 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   const int b = seq_of_row(a.p, row);
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
-  const int i = row - s.first;
-  if (i >= s.q) return;
-  const int m = i * a.G + head % a.G;
-  const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
+  if (row - s.first >= s.q) return;
+  const KeyRange kr = key_range(a, s, 0, 16);
   const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
   if (n > 1) join_pieces<T, DH>(a, row, head, n);               // else written where it was computed
+}
+
+// many rows of few pieces: a wavefront takes 256 / DH heads of a row, DH / 4 lanes each (24576 rows and heads of two pieces: 10.4 us
+// with a wavefront each, 5.7 so)
+template <typename T, int DH, int ROWS>
+__global__ __launch_bounds__(256) void attention_paged_join_rows_kernel(AttnArgs a) {
+  constexpr int L = DH / 4, HEADS = 64 / L;
+  const int lane = threadIdx.x & 63, dim = lane % L * 4;
+  const int idx = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_row = (a.H + HEADS - 1) / HEADS;
+  const int row = idx / per_row, head = (idx - row * per_row) * HEADS + lane / L;
+  if (row >= a.p.n_rows) return;
+  const int b = seq_of_row(a.p, row);
+  if (b < 0) return;
+  const SeqRange s = seq_range(a.p, b);
+  const int i = row - s.first;
+  if (i >= s.q || head >= a.H) return;
+  const int h = token_of(a, head), m = i * a.G + head - h * a.G;
+  const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
+  const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
+  if (n <= 1) return;
+  const size_t rh = (size_t)row * a.H + head;
+  const float2* ml = a.part_ml + rh * a.n_split;
+  const float* po = a.part_o + rh * a.n_split * DH + dim;
+  float top = -INFINITY, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < n; ++j) top = fmaxf(top, ml[j].x);
+  const float top_use = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) {
+    const float2 v = ml[j];
+    const float4 p = *reinterpret_cast<const float4*>(po + (size_t)j * DH);
+    const float f = __builtin_amdgcn_exp2f(v.x - top_use);
+    l += f * v.y;
+    y[0] += f * p.x; y[1] += f * p.y; y[2] += f * p.z; y[3] += f * p.w;
+  }
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) y[t] *= inv;
+  store_vec<T, 4>((T*)a.out + (size_t)row * a.ld_out + head * DH + dim, y);
+  if (a.lse && dim == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
 }
 
 // ---- many rows in bf16: 128 rows a workgroup share key tiles in LDS -----------------------------------------------------
@@ -1085,7 +1123,9 @@ struct Plan {
 // How a call is cut.  Up to 16 rows a head (single tokens above all): 16-row products with the keys dealt to wavefronts.  More
 // rows in bf16 share key tiles in LDS, in fp32 (bound by the matrix instructions of that type) 64 rows walk the keys together.
 // The key axis is cut where there are too few row blocks to fill the chip.
-Plan make_plan(int dtype, int n_rows, int n_seqs, int n_kv, int G, int max_new, int max_len) {
+// span: the longest range of keys that a row block can see (a window may make it shorter than max_len); workspaces are sized
+// for span = max_len, and a shorter one never gets more pieces.
+Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G, int max_new, int max_len, int span) {
   Plan p{};
   const int64_t rows = (int64_t)max_new * G;
   p.tile = rows > 16 && dtype == LLMC_BF16;
@@ -1094,20 +1134,29 @@ Plan make_plan(int dtype, int n_rows, int n_seqs, int n_kv, int G, int max_new, 
   p.join_rows = (int)std::min<int64_t>(rows, 16);
   p.blocks = rows <= p.rows ? n_seqs : std::min<int64_t>((rows + p.rows - 1) / p.rows * n_seqs, (int64_t)n_rows * G / p.rows + n_seqs);
   const int64_t units = std::max<int64_t>(1, p.blocks * n_kv);
-  int64_t want;                // pieces of the key axis
-  if (p.tile || p.rowsplit) {
-    want = (p.tile ? 512 : 1024) / units;
-  } else {
-    // Eight steps of a workgroup take as long as the second launch that joins pieces (one sequence of 777 tokens, 12 heads of 64: 8.0 us
-    // in one piece, 4.4 + 4.0 in seven).  From two workgroups a compute unit on, cutting gains less than that launch (64 sequences
-    // of up to 2048: 42 and 47 + 4); below, pieces even out ragged lengths (6 of up to 32768, 8 heads of 128: 1024 workgroups
-    // 106 + 4.5 us, 2048 92 + 7, 4096 93 + 10).
-    const int steps8 = 8 * 4 * (dtype == LLMC_BF16 ? 32 : 16);
-    want = max_len <= steps8 || units >= 512 ? 1 : 2048 / units;
-  }
-  want = std::max<int64_t>(1, want);
-  p.split = (int)std::max<int64_t>(256, align_up((size_t)((max_len + want - 1) / want), 128));
-  p.n_split = std::max(1, (int)((max_len + p.split - 1) / p.split));
+  const auto cut = [&](int len, int most) {
+    int64_t want;                // pieces of the key axis
+    int least = 256;             // keys of a piece
+    if (p.tile || p.rowsplit) {
+      // As many as are resident: four a compute unit, of 128-wide bf16 heads two.  Where there is a workgroup a compute unit anyway,
+      // only in pieces long enough to pay for being joined (12 chunks of up to 333 tokens over 3000, 12 heads: 59 us whole, 40 + 5 in
+      // three; 5 prompts of 1024: 24 whole, 25 + 10 in two).
+      want = (p.tile && head_dim == 128 ? 512 : 1024) / units;
+      if (units >= 256) least = 768;
+    } else {
+      // Eight steps of a workgroup take as long as the second launch that joins pieces (one sequence of 777 tokens, 12 heads of 64:
+      // 8.0 us in one piece, 4.4 + 4.0 in seven).  From two workgroups a compute unit on, cutting gains less than that launch
+      // (64 sequences of up to 2048: 42 and 47 + 4); below, pieces even out ragged lengths (6 of up to 32768, 8 heads of 128: 1024
+      // workgroups 106 + 4.5 us, 2048 92 + 7, 4096 93 + 10).
+      const int steps8 = 8 * 4 * (dtype == LLMC_BF16 ? 32 : 16);
+      want = len <= steps8 || units >= 512 ? 1 : 2048 / units;
+    }
+    want = std::max<int64_t>(1, std::min<int64_t>({want, most, len / least}));
+    p.split = (int)std::max<int64_t>(256, align_up((size_t)((len + want - 1) / want), 128));
+    p.n_split = std::max(1, (int)((len + p.split - 1) / p.split));
+  };
+  cut(max_len, max_len);
+  if (span < max_len) cut(span, p.n_split);
   // Wavefronts that sum weights: two a SIMD at least as long as each has 128 rows, and none with many more than 256 rows: the first keys
   // of a long chunk would keep the call waiting (16 prompts of 1024 tokens, 12 heads: 64 us in one share, 54 in four).
   const int64_t waves = (int64_t)n_seqs * n_kv * ((max_len + 63) / 64);
@@ -1160,10 +1209,12 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
   LLMC_LAUNCH_CHECK("attention_paged");
   if (p.n_split > 1 && !a.scores) {
     ProfScope ps_("attention_paged_join_kernel", st);
-    const dim3 jg((unsigned)(((int64_t)a.p.n_rows * a.H + 3) / 4));
-    if (p.rows == 128) LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 128>), jg, dim3(256), 0, st, a);
-    else if (p.rows == 64) LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 64>), jg, dim3(256), 0, st, a);
-    else LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH, 16>), jg, dim3(256), 0, st, a);
+    constexpr int heads = 256 / DH;
+    const dim3 one((unsigned)(((int64_t)a.p.n_rows * a.H + 3) / 4));
+    const dim3 many((unsigned)(((int64_t)a.p.n_rows * ((a.H + heads - 1) / heads) + 3) / 4));
+    if (p.rows == 128) LLMC_KERNEL_GGL((attention_paged_join_rows_kernel<T, DH, 128>), many, dim3(256), 0, st, a);
+    else if (p.rows == 64) LLMC_KERNEL_GGL((attention_paged_join_rows_kernel<T, DH, 64>), many, dim3(256), 0, st, a);
+    else LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH>), one, dim3(256), 0, st, a);
     LLMC_LAUNCH_CHECK("attention_paged_join");
   }
   if (weight && a.scores) {
@@ -1191,12 +1242,12 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
 
 size_t attention_paged_ws_bytes(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len,
                                 bool weights) {
-  const Plan p = make_plan(dtype, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len);
+  const Plan p = make_plan(dtype, head_dim, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len, max_len);
   return ws_layout(p, n_rows, H, head_dim, n_seqs, n_kv, max_len, weights).total;
 }
 
-bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
-  const Plan p = make_plan(dtype, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len);
+bool attention_paged_grid_ok(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
+  const Plan p = make_plan(dtype, head_dim, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len, max_len);
   const int64_t most = 0x7FFFFFFF;
   return p.blocks <= 65535 && p.n_split <= 65535 && (int64_t)n_rows * H <= most && p.blocks * n_kv <= most / p.n_split &&
          (!weights || (int64_t)((max_len + 15) / 16) <= most / n_seqs);
@@ -1205,13 +1256,16 @@ bool attention_paged_grid_ok(int dtype, int n_kv, int H, int n_rows, int n_seqs,
 llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at,
                                      const void* q, int64_t ld_q, void* out, int64_t ld_out, void* ws, hipStream_t st) {
   if (bt->n_rows == 0) return LLMC_OK;
-  const Plan p = make_plan(kv->dtype, bt->n_rows, bt->n_seqs, kv->n_kv_heads, at->n_heads / kv->n_kv_heads, bt->max_new, bt->max_len);
+  const int G = at->n_heads / kv->n_kv_heads;
+  const bool by_slot = at->window > 0 && !bt->d_pos;             // a block of 128 rows sees a window behind each, rounded to 64 keys
+  const int span = by_slot ? (int)std::min<int64_t>(bt->max_len, (int64_t)at->window + std::min(bt->max_new, 127 / G + 1) + 63) : bt->max_len;
+  const Plan p = make_plan(kv->dtype, kv->head_dim, bt->n_rows, bt->n_seqs, kv->n_kv_heads, G, bt->max_new, bt->max_len, span);
   const bool weights = bt->d_weight && at->accumulate;
   const Layout l = ws_layout(p, bt->n_rows, at->n_heads, kv->head_dim, bt->n_seqs, kv->n_kv_heads, bt->max_len, weights);
   AttnArgs a{};
   a.p = paged_args(kv, bt);
   a.q = q; a.out = out; a.k = kv->d_k; a.v = kv->d_v; a.ld_q = ld_q; a.ld_out = ld_out;
-  a.H = at->n_heads; a.G = at->n_heads / kv->n_kv_heads;
+  a.H = at->n_heads; a.G = G;
   a.g_magic = row_magic(a.G); a.split_magic = row_magic(p.split);
   a.softcap = at->softcap;
   a.mul = at->scale * kLog2e;
