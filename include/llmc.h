@@ -608,7 +608,8 @@ typedef struct {
  * apart (multiples of 16 bytes), element type of the cache; d_out must not overlap d_q or the pages.
  * Softmax statistics, sums and accumulated weights are fp32 in a fixed order (no atomics); with bf16 elements the weights of
  * the value product are rounded to bf16.  What slots beyond a sequence's length hold does not matter.
- * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.
+ * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.  (With accumulate and
+ * up to 16 rows a key/value head -- new tokens times query heads of a group -- it holds a score a query head and slot.)
  * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite), SHAPE (head
  * counts, strides, alignment, bounds), DTYPE, WORKSPACE.
  */

@@ -517,6 +517,7 @@ llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch
   LLMC_TRY(check_attn(kv, batch, attn));
   LLMC_TRY(check_attn_values(batch, attn));
   REQUIRE((d_q && d_out) || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "queries or outputs are NULL");
+  REQUIRE(d_q != d_out || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "d_q and d_out must not overlap");
   const int64_t row = (int64_t)attn->n_heads * kv->head_dim, per = 16 / (int64_t)elem_size(kv->dtype);
   REQUIRE(ld_q >= row && ld_out >= row && ld_q % per == 0 && ld_out % per == 0, LLMC_ERR_SHAPE,
           "row strides must be at least n_heads * head_dim and multiples of 16 bytes");

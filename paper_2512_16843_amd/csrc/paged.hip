@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // The choice: one workgroup per sequence.  A token's key is 64 bits (protected flag, weight, position); the (n - k)-th smallest is
 // narrowed by digits of 11 bits, most significant first, a histogram in LDS a digit, until at most 64 keys share the digits
 // so far (two digits, as weights go); a wavefront then ranks those by key and slot.  Holes and movers are numbered by counts
-// of ballots.  Up to 32768 tokens the keys are read once and stay in registers.  Bound: latency, one workgroup's chain of loads and
+// of ballots.  Up to 24576 tokens the keys are read once and stay in registers.  Bound: latency, one workgroup's chain of loads and
 // barriers (64 sequences of 1040 tokens 8.6 us, 8 of up to 8192 14; eight digits of 8 bits and keys read in each pass 17.4 and 42).
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kDigit = 11, kBins = 1 << kDigit;
 
@@ -381,7 +381,7 @@ llmc_status_t launch_kv_evict(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* b
     const dim3 grid((unsigned)bt->n_seqs), block(kSelThreads);
     if (bt->max_len <= 2 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<2>, grid, block, 0, st, a);
     else if (bt->max_len <= 8 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<8>, grid, block, 0, st, a);
-    else if (bt->max_len <= 32 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<32>, grid, block, 0, st, a);
+    else if (bt->max_len <= 24 * kSelThreads) LLMC_KERNEL_GGL(kv_evict_select_kernel<24>, grid, block, 0, st, a);
     else LLMC_KERNEL_GGL(kv_evict_select_kernel<0>, grid, block, 0, st, a); }
   LLMC_LAUNCH_CHECK("kv_evict_select");
   const int vec_shift = log2_of(kv->head_dim * (int)elem_size(kv->dtype) / 16);

@@ -211,8 +211,10 @@ class PagedStack:
         """``h`` [sum(new), d]: the embedded new tokens, ``new[b]`` of them for sequence b, in order.  Returns their outputs.
         Raises before anything is enqueued, and changes nothing, if a sequence or the pool would overflow."""
         cfg, B = self.cfg, self.n_seqs
-        if len(new) != B or min(new) < 0 or h.dim() != 2 or h.shape[0] != sum(new):
+        if len(new) != B or min(new) < 0 or tuple(h.shape) != (sum(new), cfg.d):
             raise ValueError("one count for each sequence, and a row of h for each new token")
+        if h.dtype != cfg.torch_dtype or not h.is_contiguous() or not h.is_cuda:
+            raise ValueError("h must be contiguous %s on the GPU" % cfg.torch_dtype)
         if sum(new) == 0:
             return h.new_empty(h.shape)
         lens = [n + q for n, q in zip(self.lengths, new)]

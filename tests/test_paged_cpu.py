@@ -84,7 +84,7 @@ def test_refusals_of_append(lib):
 
 def test_refusals_of_attention(lib):
     big = 1 << 30
-    def call(k=kv(), b=batch(), a=attn(), q=P, ldq=256, out=P, ldo=256, ws=P, n=big):
+    def call(k=kv(), b=batch(), a=attn(), q=P, ldq=256, out=2 * P, ldo=256, ws=P, n=big):
         return lib.llmc_attention_paged(ref(k), ref(b), ref(a), q, ldq, out, ldo, ws, n, None)
     for k, st in BAD_KV:
         assert call(k=k) == st, lib.llmc_last_error()
@@ -93,7 +93,7 @@ def test_refusals_of_attention(lib):
     for a, st in BAD_ATTN:
         assert call(a=a) == st, lib.llmc_last_error()
     assert call(a=attn(accumulate=1), b=batch(d_weight=None)) == llmc.ERR_INVALID_ARG
-    assert call(q=None) == llmc.ERR_INVALID_ARG and call(out=None) == llmc.ERR_INVALID_ARG
+    assert call(q=None) == llmc.ERR_INVALID_ARG and call(out=None) == llmc.ERR_INVALID_ARG and call(out=P) == llmc.ERR_INVALID_ARG
     assert call(ldq=248) == llmc.ERR_SHAPE and call(ldo=260) == llmc.ERR_SHAPE
     assert call(q=P + 8) == llmc.ERR_SHAPE and call(ws=P + 8) == llmc.ERR_SHAPE
     assert call(ws=None) == llmc.ERR_WORKSPACE and call(n=8) == llmc.ERR_WORKSPACE
