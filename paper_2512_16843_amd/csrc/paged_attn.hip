@@ -34,8 +34,8 @@ struct AttnArgs {
   int32_t H, G;
   uint64_t g_magic, split_magic;   // row_magic of G and of split
   float softcap;
-  float mul, add;              // a score in base 2 from a product (scale * log2(e), 0) or, capped, from y (2 c, c; c = softcap * log2(e))
-  float cap_in;                // scale * 2 log2(e) / softcap
+  float mul, add;              // a score in base 2 from a product (scale * log2(e), 0) or from what cap_scores makes of it
+  float cap_in;                // scale / softcap; fast: times 2 log2(e)
   int32_t window;              // 0: none
   const float* slopes;
   const int32_t* pos;          // NULL: slots are positions
@@ -83,19 +83,38 @@ __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, const SeqRange&
   return r;
 }
 
-// A capped score in base 2 is c + 2 c y with y = -1 / (1 + 2^(2 log2(e) x / c)): one exponential and one reciprocal, exact at
-// both ends, and y takes the place of the product in the one fma of the exponent.
-template <int N>
+// Capped scores take the place of the products in the one fma of the exponent.
+//   FAST, for the 128-row blocks whose weights are rounded to bf16: c + 2 c y with y = -1 / (1 + 2^(2 log2(e) x / c)), one exponential
+//   and one reciprocal, exact at both ends; near zero it is off by 2^-23 c, far below that rounding.
+//   Else, where memory is the bound or the result has 24 bits: c t with t = tanh(x / c) to the last bits, (1 - E) / (1 + E) with
+//   E = 2^(-2 log2(e) |x| / c), and below 0.45 the power series, whose first term left out is 2 * 10^-8 of the sum there.
+template <bool FAST, int N>
 __device__ __forceinline__ void cap_scores(const AttnArgs& a, float (&y)[N]) {
+  if constexpr (FAST) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) y[i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(y[i] * a.cap_in));
+    for (int i = 0; i < N; ++i) y[i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(y[i] * a.cap_in));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float z = y[i] * a.cap_in, u = fabsf(z), q = u * u;
+      const float e = __builtin_amdgcn_exp2f(u * (-2.f * kLog2e));
+      const float big = (1.f - e) * __builtin_amdgcn_rcpf(1.f + e);
+      float p = 21844.f / 6081075.f;
+      p = fmaf(p, q, -1382.f / 155925.f);
+      p = fmaf(p, q, 62.f / 2835.f);
+      p = fmaf(p, q, -17.f / 315.f);
+      p = fmaf(p, q, 2.f / 15.f);
+      p = fmaf(p, q, -1.f / 3.f);
+      y[i] = copysignf(u < 0.45f ? fmaf(u * q, p, u) : big, z);
+    }
+  }
 }
 
 // Scores in base 2 from N products, lowered by slope2 * away(i) and hidden at and beyond the window.  The branches are uniform
 // and outside the loops.
-template <int N, typename Away>
+template <bool FAST, int N, typename Away>
 __device__ __forceinline__ void bias_scores(const AttnArgs& a, float (&x)[N], Away away, float slope2) {
-  if (a.softcap > 0.f) cap_scores(a, x);
+  if (a.softcap > 0.f) cap_scores<FAST>(a, x);
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = fmaf(-slope2, (float)away(i), fmaf(x[i], a.mul, a.add));
   if (a.window > 0) {
@@ -398,10 +417,10 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     fetch_k(st, kb + STEP);
     ask_pages(kb + 2 * STEP);
     if (FEAT == 2) {
-      bias_scores(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
+      bias_scores<false>(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
     } else if (FEAT == 1) {
       const int away0 = t_slot - kb - 4 * g;
-      bias_scores(a, x, [&](int i) { return away0 - 16 * (i >> 2) - (i & 3); }, slope);
+      bias_scores<false>(a, x, [&](int i) { return away0 - 16 * (i >> 2) - (i & 3); }, slope);
     } else {
 #pragma unroll
       for (int i = 0; i < SUB * 4; ++i) x[i] *= a.mul;
@@ -773,14 +792,14 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
     const auto off = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
     const int key0 = kb + half * 4, away0 = t_slot - key0;
     if (FEAT == 2) {
-      bias_scores(a, x, [&](int i) { return t_pos - tile_pos[half * 4 + off(i)]; }, slope);
+      bias_scores<true>(a, x, [&](int i) { return t_pos - tile_pos[half * 4 + off(i)]; }, slope);
     } else if (FEAT == 1) {
-      if (a.softcap > 0.f) cap_scores(a, x);
+      if (a.softcap > 0.f) cap_scores<true>(a, x);
       const float base = (float)away0;                            // distances below 2^24 are exact
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = fmaf(-slope, base - (float)off(i), fmaf(x[i], a.mul, a.add));
     } else if (a.softcap > 0.f) {
-      cap_scores(a, x);
+      cap_scores<true>(a, x);
     }
     if (FEAT != 2 && kb < w_first) {
 #pragma unroll
@@ -967,9 +986,9 @@ __global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = sc[r];
         if (FEAT == 2) {
-          bias_scores(a, x, [&](int r) { return R.t_pos[i] - key_pos[u][r]; }, R.slope[i]);
+          bias_scores<false>(a, x, [&](int r) { return R.t_pos[i] - key_pos[u][r]; }, R.slope[i]);
         } else {
-          if (a.softcap > 0.f) cap_scores(a, x);
+          if (a.softcap > 0.f) cap_scores<false>(a, x);
           if (FEAT == 1) {
             const float base = (float)(R.t_slot[i] - key0);
 #pragma unroll
@@ -1181,6 +1200,17 @@ Layout ws_layout(const Plan& p, int n_rows, int H, int DH, int n_seqs, int n_kv,
   return l;
 }
 
+void set_scores(AttnArgs& a, const llmc_attn_desc_t* at, bool fast_cap) {
+  if (at->softcap > 0.f) {
+    const float c2 = at->softcap * kLog2e;
+    a.cap_in = (float)((fast_cap ? 2.0 * 1.4426950408889634 : 1.0) * at->scale / at->softcap);
+    a.mul = fast_cap ? 2.f * c2 : c2;
+    a.add = fast_cap ? c2 : 0.f;
+  } else {
+    a.mul = at->scale * kLog2e;
+  }
+}
+
 template <int DH, int FEAT>
 llmc_status_t launch_tile(const AttnArgs& a, dim3 grid, hipStream_t st) {
   static std::atomic<bool> lds_set[64];
@@ -1191,7 +1221,8 @@ llmc_status_t launch_tile(const AttnArgs& a, dim3 grid, hipStream_t st) {
 }
 
 template <typename T, int DH, int FEAT>
-llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* weight, hipStream_t st) {
+llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, float* sums, float* weight, hipStream_t st) {
+  set_scores(a, at, p.tile);
   const dim3 grid((unsigned)a.p.n_kv, (unsigned)p.n_split, (unsigned)p.blocks);
   {
     ProfScope ps_("attention_paged_kernel", st);
@@ -1225,6 +1256,7 @@ llmc_status_t launch_t(const AttnArgs& a, const Plan& p, float* sums, float* wei
     LLMC_LAUNCH_CHECK("attention_paged_score_weights");
   } else if (weight) {
     constexpr int keys = WeightCfg<T, DH>::KEYS;
+    set_scores(a, at, false);
     { ProfScope ps_("attention_paged_weight_kernel", st);
       const dim3 wg((unsigned)((a.p.max_len + keys - 1) / keys * a.p.n_seqs), (unsigned)a.p.n_kv, (unsigned)p.shares);
       if (FEAT == 1 && !a.slopes) LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, 0>), wg, dim3(64), 0, st, a, sums);
@@ -1268,12 +1300,6 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   a.H = at->n_heads; a.G = G;
   a.g_magic = row_magic(a.G); a.split_magic = row_magic(p.split);
   a.softcap = at->softcap;
-  a.mul = at->scale * kLog2e;
-  if (at->softcap > 0.f) {
-    a.cap_in = (float)(2.0 * 1.4426950408889634 * at->scale / at->softcap);
-    a.add = at->softcap * kLog2e;
-    a.mul = 2.f * a.add;
-  }
   a.window = at->window; a.slopes = at->d_slopes;
   a.pos = (at->window > 0 || at->d_slopes) ? bt->d_pos : nullptr;
   a.split = p.split; a.n_split = p.n_split;
@@ -1289,9 +1315,9 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   float* weight = weights ? bt->d_weight : nullptr;
   const int feat = a.pos ? 2 : at->softcap > 0.f || at->window > 0 || at->d_slopes ? 1 : 0;
 #define LLMC_PAGED(T_, DH_)                                                  \
-  return feat == 2   ? launch_t<T_, DH_, 2>(a, p, sums, weight, st)          \
-         : feat == 1 ? launch_t<T_, DH_, 1>(a, p, sums, weight, st)          \
-                     : launch_t<T_, DH_, 0>(a, p, sums, weight, st)
+  return feat == 2   ? launch_t<T_, DH_, 2>(a, at, p, sums, weight, st)          \
+         : feat == 1 ? launch_t<T_, DH_, 1>(a, at, p, sums, weight, st)          \
+                     : launch_t<T_, DH_, 0>(a, at, p, sums, weight, st)
   if (kv->dtype == LLMC_BF16) {
     if (kv->head_dim == 64) LLMC_PAGED(bf16_t, 64);
     LLMC_PAGED(bf16_t, 128);
