@@ -1155,13 +1155,15 @@ Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G,
   const int64_t units = std::max<int64_t>(1, p.blocks * n_kv);
   const auto cut = [&](int len, int most) {
     int64_t want;                // pieces of the key axis
-    int least = 256;             // keys of a piece
+    int least = p.rowsplit && head_dim == 128 ? 128 : 256;             // keys of a piece
     if (p.tile || p.rowsplit) {
-      // As many as are resident: four a compute unit, of 128-wide bf16 heads two.  Where there is a workgroup a compute unit anyway,
+      // bf16: as many as are resident, four a compute unit, of 128-wide heads two.  Where there is a workgroup a compute unit anyway,
       // only in pieces long enough to pay for being joined (12 chunks of up to 333 tokens over 3000, 12 heads: 59 us whole, 40 + 5 in
       // three; 5 prompts of 1024: 24 whole, 25 + 10 in two).
-      want = (p.tile && head_dim == 128 ? 512 : 1024) / units;
-      if (units >= 256) least = 768;
+      // fp32: twice as many, a step is long there (8 chunks of up to 256 tokens over 1024, 12 heads of 64: 66 us whole, 45 + 5 in
+      // pieces; 4 of them with heads of 128: 68 + 5.5 us in pieces of 256 keys, 58 + 7 of 128).
+      want = (p.rowsplit ? 2048 : head_dim == 128 ? 512 : 1024) / units;
+      if (p.tile && units >= 256) least = 768;
     } else {
       // Eight steps of a workgroup take as long as the second launch that joins pieces (one sequence of 777 tokens, 12 heads of 64:
       // 8.0 us in one piece, 4.4 + 4.0 in seven).  From two workgroups a compute unit on, cutting gains less than that launch
@@ -1171,7 +1173,7 @@ Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G,
       want = len <= steps8 || units >= 512 ? 1 : 2048 / units;
     }
     want = std::max<int64_t>(1, std::min<int64_t>({want, most, len / least}));
-    p.split = (int)std::max<int64_t>(256, align_up((size_t)((len + want - 1) / want), 128));
+    p.split = (int)std::max<int64_t>(least, align_up((size_t)((len + want - 1) / want), 128));
     p.n_split = std::max(1, (int)((len + p.split - 1) / p.split));
   };
   cut(max_len, max_len);
