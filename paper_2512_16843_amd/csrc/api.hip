@@ -482,8 +482,9 @@ static llmc_status_t check_attn(const llmc_kv_desc_t* kv, const llmc_kv_batch_t*
   return LLMC_OK;
 }
 static llmc_status_t check_attn_values(const llmc_kv_batch_t* bt, const llmc_attn_desc_t* at) {
-  REQUIRE(at->scale > 0.f && isfinite(at->scale), LLMC_ERR_INVALID_ARG, "scale must be positive and finite");
-  REQUIRE(at->softcap >= 0.f && isfinite(at->softcap), LLMC_ERR_INVALID_ARG, "softcap must be finite and not negative");
+  REQUIRE(at->scale > 0.f && isfinite(2.f * at->scale), LLMC_ERR_INVALID_ARG, "scale must be positive and finite");
+  REQUIRE(at->softcap >= 0.f && isfinite(4.f * at->softcap), LLMC_ERR_INVALID_ARG, "softcap must be finite and not negative");
+  REQUIRE(at->softcap == 0.f || isfinite(4.f * at->scale / at->softcap), LLMC_ERR_INVALID_ARG, "scale / softcap overflows");
   REQUIRE(at->window >= 0, LLMC_ERR_INVALID_ARG, "window must not be negative");
   REQUIRE(!at->accumulate || bt->d_weight, LLMC_ERR_INVALID_ARG, "accumulate needs d_weight");
   return LLMC_OK;

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
   const int i = row - s.first, slot = s.len - s.q + i;
-  if (i >= s.q || slot < 0) return;
+  if ((uint32_t)i >= (uint32_t)s.q || slot < 0) return;
   const int page = page_of(a.p, b, slot);
   const int nv = a.p.n_kv << a.vec_shift, off = slot & ((1 << a.p.page_shift) - 1);
   if (page >= 0) {

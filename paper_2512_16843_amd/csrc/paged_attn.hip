@@ -84,8 +84,10 @@ __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, const SeqRange&
 }
 
 // Capped scores take the place of the products in the one fma of the exponent.
-//   FAST, for the 128-row blocks whose weights are rounded to bf16: c + 2 c y with y = -1 / (1 + 2^(2 log2(e) x / c)), one exponential
-//   and one reciprocal, exact at both ends; near zero it is off by 2^-23 c, far below that rounding.
+//   FAST, for the 128-row blocks whose weights are rounded to bf16: c + 2 c y with y = -1 / (1 + 2^(2 log2(e) x / c)), one exponential and
+//   one reciprocal, exact at both ends; near zero it is off by 2^-23 c, far below that rounding for c up to 1024.  The normalisers
+//   of weights that are accumulated in fp32 take it up to 64: 2^-17 at most, 2^-23 as the keys' errors average (a chunk capped at 30,
+//   12 heads of 64: 45 us, 64 with the exact form).
 //   Else, where memory is the bound or the result has 24 bits: c t with t = tanh(x / c) to the last bits, (1 - E) / (1 + E) with
 //   E = 2^(-2 log2(e) |x| / c), and below 0.45 the power series, whose first term left out is 2 * 10^-8 of the sum there.
 template <bool FAST, int N>
@@ -112,9 +114,9 @@ __device__ __forceinline__ void cap_scores(const AttnArgs& a, float (&y)[N]) {
 
 // Scores in base 2 from N products, lowered by slope2 * away(i) and hidden at and beyond the window.  The branches are uniform
 // and outside the loops.
-template <bool FAST, int N, typename Away>
+template <int N, typename Away>
 __device__ __forceinline__ void bias_scores(const AttnArgs& a, float (&x)[N], Away away, float slope2) {
-  if (a.softcap > 0.f) cap_scores<FAST>(a, x);
+  if (a.softcap > 0.f) cap_scores<false>(a, x);
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = fmaf(-slope2, (float)away(i), fmaf(x[i], a.mul, a.add));
   if (a.window > 0) {
@@ -289,7 +291,7 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int blk, int n_
 // long axis are better mixed (6 sequences of up to 32768, 8 heads of 128: 91 us, 100 in order).
 __device__ __forceinline__ int nth_longest(const PagedArgs& p, int n) {
   const int lane = threadIdx.x & 63, first = n & ~63;
-  const int len = first + lane < p.n_seqs ? p.length[first + lane] : -1;
+  const int len = first + lane < p.n_seqs ? max(p.length[first + lane], 0) : -1;
   int rank = 0;
 #pragma unroll 8
   for (int k = 0; k < 64; ++k) {
@@ -417,10 +419,10 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
     fetch_k(st, kb + STEP);
     ask_pages(kb + 2 * STEP);
     if (FEAT == 2) {
-      bias_scores<false>(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
+      bias_scores(a, x, [&](int i) { return t_pos - key_pos[i]; }, slope);
     } else if (FEAT == 1) {
       const int away0 = t_slot - kb - 4 * g;
-      bias_scores<false>(a, x, [&](int i) { return away0 - 16 * (i >> 2) - (i & 3); }, slope);
+      bias_scores(a, x, [&](int i) { return away0 - 16 * (i >> 2) - (i & 3); }, slope);
     } else {
 #pragma unroll
       for (int i = 0; i < SUB * 4; ++i) x[i] *= a.mul;
@@ -580,7 +582,7 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   const int b = seq_of_row(a.p, row);
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
-  if (row - s.first >= s.q) return;
+  if ((uint32_t)(row - s.first) >= (uint32_t)s.q) return;
   const KeyRange kr = key_range(a, s, 0, 16);
   const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
   if (n > 1) join_pieces<T, DH>(a, row, head, n);               // else written where it was computed
@@ -599,7 +601,7 @@ __global__ __launch_bounds__(256) void attention_paged_join_rows_kernel(AttnArgs
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
   const int i = row - s.first;
-  if (i >= s.q || head >= a.H) return;
+  if ((uint32_t)i >= (uint32_t)s.q || head >= a.H) return;
   const int h = token_of(a, head), m = i * a.G + head - h * a.G;
   const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
   const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
@@ -632,7 +634,8 @@ __global__ __launch_bounds__(256) void attention_paged_join_rows_kernel(AttnArgs
 // transposing reads (a group of 16 lanes gets 4 keys of 16 dims, 4 keys a lane).  The 16-byte chunks of a row are XOR-swizzled by
 // the row, on the global side: 16 consecutive rows then offer one chunk in 16 places (the keys' 16-byte reads), and four
 // consecutive rows four neighbouring chunks in 4 different quarters of the banks (the values' transposing reads).
-// FEAT 0: plain or capped scores, with or without a window; 1: bias by distance; 2: positions that are not the slots' numbers.
+// FEAT 0: plain or (FAST) capped scores, with or without a window; 1: bias by distance, or exact capping; 2: positions that are not
+// the slots' numbers.
 template <int DH>
 struct TileCfg {
   static constexpr int KT = 64, ROWS = 128;
@@ -792,9 +795,9 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
     const auto off = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
     const int key0 = kb + half * 4, away0 = t_slot - key0;
     if (FEAT == 2) {
-      bias_scores<true>(a, x, [&](int i) { return t_pos - tile_pos[half * 4 + off(i)]; }, slope);
+      bias_scores(a, x, [&](int i) { return t_pos - tile_pos[half * 4 + off(i)]; }, slope);
     } else if (FEAT == 1) {
-      if (a.softcap > 0.f) cap_scores<true>(a, x);
+      if (a.softcap > 0.f) cap_scores<false>(a, x);
       const float base = (float)away0;                            // distances below 2^24 are exact
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = fmaf(-slope, base - (float)off(i), fmaf(x[i], a.mul, a.add));
@@ -986,7 +989,7 @@ __global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = sc[r];
         if (FEAT == 2) {
-          bias_scores<false>(a, x, [&](int r) { return R.t_pos[i] - key_pos[u][r]; }, R.slope[i]);
+          bias_scores(a, x, [&](int r) { return R.t_pos[i] - key_pos[u][r]; }, R.slope[i]);
         } else {
           if (a.softcap > 0.f) cap_scores<false>(a, x);
           if (FEAT == 1) {
@@ -1224,7 +1227,8 @@ llmc_status_t launch_tile(const AttnArgs& a, dim3 grid, hipStream_t st) {
 
 template <typename T, int DH, int FEAT>
 llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, float* sums, float* weight, hipStream_t st) {
-  set_scores(a, at, p.tile);
+  const bool fast_cap = p.tile && FEAT == 1 && !a.slopes && at->softcap <= (weight ? 64.f : 1024.f);
+  set_scores(a, at, fast_cap);
   const dim3 grid((unsigned)a.p.n_kv, (unsigned)p.n_split, (unsigned)p.blocks);
   {
     ProfScope ps_("attention_paged_kernel", st);
@@ -1233,7 +1237,7 @@ llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, fl
       const size_t lds = (size_t)4 * p.join_rows * (DH + 4 + 2) * 4;
       LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, false>), grid, dim3(256), lds, st, a);
     } else if constexpr (sizeof(T) == 2) {
-      if (FEAT == 1 && !a.slopes) LLMC_TRY((launch_tile<DH, 0>(a, grid, st)));
+      if (FEAT == 1 && !a.slopes && (fast_cap || at->softcap == 0.f)) LLMC_TRY((launch_tile<DH, 0>(a, grid, st)));
       else LLMC_TRY((launch_tile<DH, FEAT>(a, grid, st)));
     } else {
       LLMC_KERNEL_GGL((attention_paged_rows_kernel<T, DH, FEAT, true>), grid, dim3(256), 0, st, a);

@@ -515,7 +515,7 @@ def _rows(t: torch.Tensor, heads: int, head_dim: int, dtype: torch.dtype, dev: i
         _refuse(ERR_SHAPE, "%s: the heads of a row must be contiguous" % what)
     if t.get_device() != dev:
         _refuse(ERR_INVALID_ARG, "%s is on %s, the pages are on device %d" % (what, t.device, dev))
-    return t.data_ptr(), (stride[0] if shape[0] > 1 else max(heads * head_dim, stride[0]))
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * head_dim)
 
 
 def _kv_desc(k_pages: torch.Tensor, v_pages: torch.Tensor, dev: int) -> KvDesc:

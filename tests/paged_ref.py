@@ -34,8 +34,9 @@ def tokens(pages, table, b, n):
     return x.permute(1, 0, 2, 3).reshape(pages.shape[1], -1, pages.shape[3])[:, :n]
 
 
-def attention(q, k, v, table, lens, starts, pos=None, scale=None, softcap=0.0, window=0, slopes=None):
-    """(out, bound of out, weights per sequence, bound of the weights) in 64 bits."""
+def attention(q, k, v, table, lens, starts, pos=None, scale=None, softcap=0.0, window=0, slopes=None, cap_rel=None):
+    """(out, bound of out, weights per sequence, bound of the weights) in 64 bits.  cap_rel: a bound of the capping's error relative
+    to the capped score, where it is not one relative to the cap."""
     H, dh = q.shape[1], q.shape[2]
     kv = k.shape[1]
     G = H // kv
@@ -66,7 +67,8 @@ def attention(q, k, v, table, lens, starts, pos=None, scale=None, softcap=0.0, w
                 dx = (dh + 8) * f * mag
                 if softcap:
                     x = softcap * torch.tanh(x / softcap)
-                    dx = dx + softcap * 2.0 ** -21                  # one exponential, one quotient, values up to 2 * softcap
+                    # one exponential, one quotient, values up to 2 * softcap
+                    dx = dx + (softcap * 2.0 ** -21 if cap_rel is None else cap_rel * x.abs())
                 if slopes is not None:
                     bias = slopes[h].double() * away
                     x = x - bias

@@ -74,9 +74,9 @@ class Case:
         torch.cuda.synchronize()
         return out.cpu()
 
-    def check(self, got):
+    def check(self, got, **more):
         want, tol, ws, wt = R.attention(self.q, self.k, self.v, self.table, self.lens, self.starts, pos=self.pos,
-                                        slopes=self.slopes, **self.opt)
+                                        slopes=self.slopes, **self.opt, **more)
         end = self.starts[-1]
         bad = (got[:end].double() - want[:end]).abs() - tol[:end]
         assert torch.isfinite(got[:end].double()).all()
@@ -191,6 +191,55 @@ def test_scores_at_the_ends_of_the_range(L, dtype, news):
     c.check(c.gpu())
     c.q.zero_()
     c.check(c.gpu())
+
+
+@pytest.mark.parametrize("dtype,weights", [("bf16", False), ("bf16", True), ("f32", True)])
+@pytest.mark.parametrize("softcap", [1.0, 50.0, 2000.0, 1e6])
+@pytest.mark.parametrize("news", [[1, 1], [200, 40]])
+def test_capping_is_exact_however_far_the_cap(L, dtype, weights, softcap, news):
+    """Roundings of tanh(z), z = x / cap, in half steps f = 2^-24 relative to the result, |z| >= 0.45, E = e^(-2 |z|) <= 0.41:
+    z itself 2 (its factor t' z / t is below one), the exponent 1 + 1 more of 2 |z| and the exponential 2 on E, all of them scaled by
+    2 E / (1 - E^2) <= 1 and |z| E small; 1 - E, 1 + E, the product 1 each, the reciprocal 2: below 12.  Below 0.45 the series: z 2,
+    six fmas whose errors shrink with z^2, the last one whole, the first term left out 2 * 10^-8 = 0.34 f: fewer.  Back to a score in base 2:
+    two more.  Only bf16 chunks round more coarsely, 2^-23 of the cap: up to a cap of 1024, where they leave no weights, or 64."""
+    fast = dtype == "bf16" and sum(news) > 32 and softcap <= (64 if weights else 1024)
+    c = Case(L, dtype, 4, 2, 64, 16, [333, 64], news, seed=8, weights=weights, softcap=softcap)
+    c.check(c.gpu(), cap_rel=None if fast else 16 * 2.0 ** -24)
+
+
+def test_more_blocks_of_a_chunk_than_lanes(L):
+    c = Case(L, "bf16", 6, 1, 64, 64, [1500, 1400], [1400, 3], seed=10)     # 8400 rows a head: 66 blocks of 128
+    c.check(c.gpu())
+
+
+@pytest.mark.parametrize("news", [1, 20])
+def test_lengths_outside_their_bounds_are_cut(L, news):
+    """Many sequences, some of whose lengths are negative or beyond max_len."""
+    g = torch.Generator().manual_seed(12)
+    lens = [int(x) for x in torch.randint(news, 49, (70,), generator=g)]
+    c = Case(L, "bf16", 4, 4, 64, 16, lens, [news] * 70, seed=11, max_len=48)
+    wrong = list(lens)
+    for b in (0, 3, 69):
+        lens[b], wrong[b] = 0, -5 - b
+    full = lens.index(48)
+    wrong[full] = 10 ** 6
+    c.lens = wrong
+    got = c.gpu(decode=news == 1)
+    c.lens = lens
+    c.check(got)
+    for b in (0, 3, 69):
+        assert (got[c.starts[b]:c.starts[b + 1]] == 0).all()
+
+
+def test_starts_that_fall_store_nothing_before_a_sequence(L):
+    g = torch.Generator().manual_seed(13)
+    k, v, table = R.make_cache(g, torch.float32, 2, 64, 16, [20, 20], fill=0.0)
+    new = torch.randn((6, 2, 64), generator=g)
+    kg, vg = k.cuda(), v.cuda()
+    L.llmc_kv_append(new.cuda(), new.cuda(), kg, vg, table.cuda(), i32([20, 20]), new_start=i32([3, 0, 6]), max_new=6)
+    torch.cuda.synchronize()
+    for got, was in ((kg, k), (vg, v)):
+        assert torch.equal(R.tokens(got.cpu(), table, 0, 20), R.tokens(was, table, 0, 20))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -68,6 +68,13 @@ BAD_ATTN = [
 ]
 
 
+def test_refusals_of_scales_and_caps_that_overflow(lib):
+    def call(a):
+        return lib.llmc_attention_paged(ref(kv()), ref(batch()), ref(a), P, 256, P + 16, 256, P, 1 << 30, None)
+    for a in (attn(scale=3e38), attn(softcap=2e38), attn(scale=1e3, softcap=1e-38)):
+        assert call(a) == llmc.ERR_INVALID_ARG, lib.llmc_last_error()
+
+
 def test_refusals_of_append(lib):
     def call(k=kv(), b=batch(), kn=P, ldk=128, vn=P, ldv=128):
         return lib.llmc_kv_append(ref(k), ref(b), kn, ldk, vn, ldv, None, None)
