@@ -243,6 +243,49 @@ def test_starts_that_fall_store_nothing_before_a_sequence(L):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,lens", [(40, [300, 1, 64]), (130, [int(n) for n in range(1, 71)])])
+def test_single_tokens_of_many_heads_on_one_key(L, dtype, heads, lens):
+    c = Case(L, dtype, heads, 1, 64, 16, lens, [1] * len(lens), seed=heads, weights=True)
+    c.check(c.gpu(decode=True))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 1, 1], [40, 3, 100]])
+def test_a_pool_beyond_32_bits(L, dtype, news):
+    """The same pages at the end of a pool of more than 2^32 elements, and at its start: the same bits."""
+    g = torch.Generator().manual_seed(14)
+    lens, kv, dh, page = [120, 33, 200], 4, 64, 64
+    k, v, table = R.make_cache(g, DT[dtype], kv, dh, page, lens)
+    far = 2 ** 32 // (kv * dh * page) + 5
+    starts = starts_of(news)
+    q = torch.randn((starts[-1], kv, dh), generator=g).to(DT[dtype]).cuda()
+    slots = table.shape[1] * page
+    pos0 = torch.arange(slots, dtype=torch.int32).repeat(3, 1)
+    res = []
+    for shift in (0, far):
+        kp = torch.empty((k.shape[0] + shift, kv, page, dh), dtype=k.dtype, device="cuda")
+        vp = torch.empty_like(kp)
+        kp[shift:], vp[shift:] = k.cuda(), v.cuda()
+        tab = (table + shift).cuda()
+        pos, w = pos0.cuda(), torch.zeros((3, slots), device="cuda")
+        kw = dict(new_start=i32(starts), max_new=max(news))
+        L.llmc_kv_append(q, q, kp, vp, tab, i32(lens), pos=pos, weight=w, **kw)
+        ws = torch.empty((L.llmc_attention_paged_workspace_bytes(q, kp, tab, max_new=max(news), max_len=200, weights=True),),
+                         dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q)
+        L.llmc_attention_paged(q, kp, vp, tab, i32(lens), out, ws, max_len=200, weight=w, **kw)
+        left = i32([0, 0, 0])
+        ws = torch.empty((L.llmc_kv_evict_workspace_bytes(tab, 200),), dtype=torch.uint8, device="cuda")
+        L.llmc_kv_evict(kp, vp, tab, i32(lens), pos, w, i32([50, 30, 20]), left, ws, max_len=200, recent=10)
+        torch.cuda.synchronize()
+        res.append([out.cpu(), w.cpu(), pos.cpu(), left.cpu()] + [R.tokens(p[shift:].cpu(), table, b, n)
+                                                                  for p in (kp, vp) for b, n in enumerate([50, 30, 20])])
+        del kp, vp
+    assert torch.isfinite(res[0][0].double()).all()
+    assert all(torch.equal(x, y) for x, y in zip(*res))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("new,vpr", [(1, 1), (7, 2), (64, 12)])
 @pytest.mark.parametrize("dh,page", [(64, 16), (128, 64)])
 def test_append(L, dtype, new, vpr, dh, page):
