@@ -1162,7 +1162,7 @@ Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G,
   const int64_t units = std::max<int64_t>(1, p.blocks * n_kv);
   const auto cut = [&](int len, int most) {
     int64_t want;                // pieces of the key axis
-    int least = p.rowsplit && head_dim == 128 ? 128 : 256;             // keys of a piece
+    int least = p.tile || (p.rowsplit && head_dim == 64) ? 256 : 128;        // keys of a piece
     if (p.tile || p.rowsplit) {
       // bf16: as many as are resident, four a compute unit, of 128-wide heads two.  Where there is a workgroup a compute unit anyway,
       // only in pieces long enough to pay for being joined (12 chunks of up to 333 tokens over 3000, 12 heads: 59 us whole, 40 + 5 in
@@ -1175,7 +1175,8 @@ Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G,
       // Eight steps of a workgroup take as long as the second launch that joins pieces (one sequence of 777 tokens, 12 heads of 64:
       // 8.0 us in one piece, 4.4 + 4.0 in seven).  From two workgroups a compute unit on, cutting gains less than that launch
       // (64 sequences of up to 2048: 42 and 47 + 4); below, pieces even out ragged lengths (6 of up to 32768, 8 heads of 128: 1024
-      // workgroups 106 + 4.5 us, 2048 92 + 7, 4096 93 + 10).
+      // workgroups 106 + 4.5 us, 2048 92 + 7, 4096 93 + 10).  Down to a step of a workgroup, two in fp32 (8 of up to 1000 in fp32, 12
+      // heads of 64, biased: 13.4 us in pieces of 256 keys, 10.5 of 128; 8 of up to 1200 in bf16: 7.7 and 6.8).
       const int steps8 = 8 * 4 * (dtype == LLMC_BF16 ? 32 : 16);
       want = len <= steps8 || units >= 512 ? 1 : 2048 / units;
     }
