@@ -610,8 +610,8 @@ typedef struct {
  * the value product are rounded to bf16.  What slots beyond a sequence's length hold does not matter.
  * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.  (With accumulate and
  * up to 16 rows a key/value head -- new tokens times query heads of a group -- it holds a score a query head and slot.)
- * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite), SHAPE (head
- * counts, strides, alignment, bounds), DTYPE, WORKSPACE.
+ * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite or so far apart that
+ * scale / softcap overflows), SHAPE (head counts, strides, alignment, bounds), DTYPE, WORKSPACE.
  */
 llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const llmc_attn_desc_t* attn,
                                    const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* d_workspace,

@@ -180,8 +180,8 @@ class PagedStack:
     """A causal decoder stack that continues sequences: every layer keeps the keys and values of earlier tokens in pages, and
     ``extend`` computes the new tokens only (a prompt, a chunk of one, or one token of each sequence; any mix).
 
-    Pages are handed out by the host from one free list; all layers share the page table and the lengths, each has its own
-    pools.  ``budget`` (with its protected ``sink`` first positions and ``recent`` last ones): after each ``extend`` every
+    Pages are handed out by the host from one free list (so ``extend`` is not for capture in a graph; the library's calls below it
+    are); all layers share the page table and the lengths, each has its own pools.  ``budget`` (with its protected ``sink`` first positions and ``recent`` last ones): after each ``extend`` every
     layer keeps that many tokens of a sequence, those that have gathered the largest attention weight in that layer."""
 
     def __init__(self, cfg: ModelConfig, weights, n_seqs: int, max_len: int, n_pages: Optional[int] = None,
@@ -271,4 +271,3 @@ class PagedStack:
         """Forgets sequence ``seq``; its pages are free for the next ``extend`` (on the same stream)."""
         self.free.extend(self.pages[seq])
         self.pages[seq], self.lengths[seq], self.next_pos[seq] = [], 0, 0
-
