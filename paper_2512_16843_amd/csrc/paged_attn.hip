@@ -41,6 +41,7 @@ struct AttnArgs {
   const int32_t* pos;          // NULL: slots are positions
   int32_t split;               // keys of one piece of a long axis, a multiple of 128
   int32_t n_split;             // pieces that the grid provides for
+  int32_t blocks;              // row blocks of all sequences, at most
   float* part_o;               // [n_rows * H, n_split, DH], not normalised
   float2* part_ml;             // [n_rows * H, n_split] (maximum in base 2, sum)
   float* lse;                  // [n_rows * H] log2 of the normaliser with the maximum in it, or NULL
@@ -238,52 +239,69 @@ template <> __device__ __forceinline__ void store_vec<bf16_t, 4>(bf16_t* p, cons
 }
 template <> __device__ __forceinline__ void store_vec<bf16_t, 8>(bf16_t* p, const float* x) { Vec16<bf16_t>::store(p, x); }
 
-// The block of rows that block `blk` of a launch over all sequences' row blocks works on (ROWS rows of one sequence's head
-// each): the sequence, and which of its blocks.  A later block of a chunk sees more keys, so the last blocks of all sequences come
-// first, then those before them (16 prompts of 1024 tokens, 12 heads: 61.7 us sequence by sequence, 51 in this order).  That
-// takes a step a level and lanes for all sequences; larger calls go sequence by sequence from the end, 64 a step.
-struct RowBlock { int b, mb; };
+// v of all lanes up to this one added up
+__device__ __forceinline__ int sum_up_to_lane(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);            // from 1, 2, 4, 8 lanes below within 16, then the last of
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);            // the 16, of the 32 before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
+// the pieces that the keys of rows [m0, m0 + rows) are cut into, as every kernel counts them
+__device__ __forceinline__ int pieces_of(const AttnArgs& a, const KeyRange& kr) {
+  return max(1, div_by(max(kr.hi - kr.lo, 0) + a.split - 1, a.split_magic));
+}
+
+// What the idx-th workgroups of a launch (one a head) work on: a block of ROWS rows of a sequence, and a piece of its keys.  A later
+// block of a chunk sees more keys, so the last blocks of all sequences come first, then those before them (16 prompts of 1024
+// tokens, 12 heads: 61.7 us sequence by sequence, 51 in this order); the pieces of a level are numbered without gaps.
+// Workgroups are dealt to compute units in turn, whatever they have to do, and idle ones in between leave the work uneven
+// (4 ragged fp32 chunks of 256 tokens over 1024, 12 heads: 33 us with gaps, 28 without; 16 of up to 300 over 4000 in bf16: 60 and
+// 46).  That takes a step a level and lanes for all sequences; larger calls go sequence by sequence from the end, 64 a step.
+struct Item { int b, mb, piece; SeqRange s; };      // b < 0: nothing
 template <int ROWS>
-__device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int blk, int n_blk) {
+__device__ __forceinline__ Item item_of(const AttnArgs& a, int idx) {
   const int lane = threadIdx.x & 63;
+  const Item none = {-1, 0, 0, {0, 0, 0}};
   if (a.by_level) {
-    const int n = lane < a.p.n_seqs ? (seq_range(a.p, lane).q * a.G + ROWS - 1) / ROWS : 0;
+    SeqRange s = {0, 0, 0};
+    if (lane < a.p.n_seqs) s = seq_range(a.p, lane);
+    const int n = (s.q * a.G + ROWS - 1) / ROWS;
     for (int level = a.by_level - 1; level >= 0; --level) {
-      const uint64_t have = __ballot(n > level);
-      const int c = __popcll(have);
-      if (blk < c) {
-        const uint64_t hit = __ballot(n > level && __popcll(have & ((1ull << lane) - 1)) == blk);
-        return RowBlock{(int)__builtin_ctzll(hit), level};
+      int count = n > level;
+      if (a.n_split > 1 && n > level) count = pieces_of(a, key_range(a, s, level * ROWS, ROWS));
+      const int upto = sum_up_to_lane(count), total = __builtin_amdgcn_readlane(upto, 63);
+      if (idx < total) {
+        const int l = (int)__builtin_ctzll(__ballot(upto > idx));
+        return Item{l, level, idx - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(count, l),
+                    {__builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.first, l), __builtin_amdgcn_readlane(s.q, l)}};
       }
-      blk -= c;
+      idx -= total;
     }
-    return RowBlock{-1, 0};
+    return none;
   }
-  blk = n_blk - 1 - blk;
+  const int at = idx / a.n_split, piece = idx - at * a.n_split, blk = a.blocks - 1 - at;
+  if (blk < 0) return none;
   if (!a.p.new_start) {
-    const int per = (a.G + ROWS - 1) / ROWS;
-    const RowBlock r = {blk / per, blk % per};
-    return r.b < a.p.n_seqs ? r : RowBlock{-1, 0};
+    const int per = (a.G + ROWS - 1) / ROWS, b = blk / per;
+    return b < a.p.n_seqs ? Item{b, blk - b * per, piece, seq_range(a.p, b)} : none;
   }
   int before = 0;
   for (int i = 0; i < a.p.n_seqs; i += 64) {
     const int b = i + lane;
-    int n = 0;
-    if (b < a.p.n_seqs) n = (seq_range(a.p, b).q * a.G + ROWS - 1) / ROWS;
-    int incl = n;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += v;
-    }
-    const uint64_t hit = __ballot(before + incl > blk);
+    const int n = b < a.p.n_seqs ? (seq_range(a.p, b).q * a.G + ROWS - 1) / ROWS : 0;
+    const int upto = before + sum_up_to_lane(n);
+    const uint64_t hit = __ballot(upto > blk);
     if (hit) {
-      const int l = __builtin_ctzll(hit);
-      return RowBlock{__builtin_amdgcn_readfirstlane(i + l),
-                      __builtin_amdgcn_readfirstlane(blk - before - (__shfl(incl, l, 64) - __shfl(n, l, 64)))};
+      const int l = (int)__builtin_ctzll(hit);
+      return Item{i + l, blk - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(n, l), piece, seq_range(a.p, i + l)};
     }
-    before += __shfl(incl, 63, 64);
+    before = __builtin_amdgcn_readlane(upto, 63);
   }
-  return RowBlock{-1, 0};
+  return none;
 }
 
 // The n-th sequence when each group of 64 is ordered by length, longest first.  In the order of the batch, lengths may repeat with the period
@@ -316,14 +334,23 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   constexpr int STEP = ROWSPLIT ? KEYS : NW * KEYS;
   extern __shared__ __attribute__((aligned(16))) float rows_lds[];          // ROWSPLIT 0: [NW][join_rows][LDO], then maxima, sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x, piece = blockIdx.y, unit = blockIdx.z;
-  const RowBlock rb = ROWSPLIT ? row_block<ROWS>(a, unit, gridDim.z) : RowBlock{a.by_length ? nth_longest(a.p, unit) : unit, 0};
-  if (rb.b < 0) return;
-  const SeqRange s = seq_range(a.p, rb.b);
+  const int h = blockIdx.x, idx = blockIdx.y + blockIdx.z * gridDim.y;
+  Item rb;
+  if (ROWSPLIT || a.n_split > 1) {
+    rb = item_of<ROWS>(a, idx);
+    if (rb.b < 0) return;
+  } else {
+    if (idx >= a.p.n_seqs) return;
+    rb.b = a.by_length ? nth_longest(a.p, idx) : idx;
+    rb.mb = rb.piece = 0;
+    rb.s = seq_range(a.p, rb.b);
+  }
+  const int piece = rb.piece;
+  const SeqRange s = rb.s;
   const int rows = s.q * a.G;
   if (rb.mb * ROWS >= rows) return;
   const KeyRange kr = key_range(a, s, rb.mb * ROWS, ROWS);
-  const int n_pieces = max(1, div_by(kr.hi - kr.lo + a.split - 1, a.split_magic));
+  const int n_pieces = pieces_of(a, kr);
   if (piece >= n_pieces) return;
   const int k_lo = kr.lo + piece * a.split;
   int k_hi = min(kr.hi, k_lo + a.split);
@@ -584,7 +611,7 @@ __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
   const SeqRange s = seq_range(a.p, b);
   if ((uint32_t)(row - s.first) >= (uint32_t)s.q) return;
   const KeyRange kr = key_range(a, s, 0, 16);
-  const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
+  const int n = pieces_of(a, kr);
   if (n > 1) join_pieces<T, DH>(a, row, head, n);               // else written where it was computed
 }
 
@@ -604,7 +631,7 @@ __global__ __launch_bounds__(256) void attention_paged_join_rows_kernel(AttnArgs
   if ((uint32_t)i >= (uint32_t)s.q || head >= a.H) return;
   const int h = token_of(a, head), m = i * a.G + head - h * a.G;
   const KeyRange kr = key_range(a, s, m / ROWS * ROWS, ROWS);
-  const int n = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
+  const int n = pieces_of(a, kr);
   if (n <= 1) return;
   const size_t rh = (size_t)row * a.H + head;
   const float2* ml = a.part_ml + rh * a.n_split;
@@ -670,14 +697,15 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
   extern __shared__ __attribute__((aligned(16))) uint16_t tile_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   // (Heads dealt so that all blocks of a sequence's head share one XCD's L2 are slower: 16 prompts of 1024 tokens, 12 heads, 68 us for 62.)
-  const int h = blockIdx.x, piece = blockIdx.y;
-  const RowBlock rb = row_block<C::ROWS>(a, blockIdx.z, gridDim.z);
+  const int h = blockIdx.x;
+  const Item rb = item_of<C::ROWS>(a, blockIdx.y + blockIdx.z * gridDim.y);
   if (rb.b < 0) return;
-  const SeqRange s = seq_range(a.p, rb.b);
+  const int piece = rb.piece;
+  const SeqRange s = rb.s;
   const int rows = s.q * a.G;
   if (rb.mb * C::ROWS >= rows) return;
   const KeyRange kr = key_range(a, s, rb.mb * C::ROWS, C::ROWS);
-  const int n_pieces = max(1, div_by(kr.hi - kr.lo + a.split - 1, a.split_magic));
+  const int n_pieces = pieces_of(a, kr);
   if (piece >= n_pieces) return;
   const int k_lo = kr.lo + piece * a.split, k_hi = min(kr.hi, k_lo + a.split);
   const int n_tiles = (k_hi - k_lo + C::KT - 1) / C::KT;
@@ -925,8 +953,9 @@ __global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, 
   constexpr int SUB = F::SUB, TILES = W::TILES, NK = TILES / SUB, RT = W::RT;
   const int lane = threadIdx.x, c = lane & 15, g = lane >> 4;
   const int h = blockIdx.y, share = blockIdx.z, shares = gridDim.z;
-  const int b = blockIdx.x % a.p.n_seqs, kb = blockIdx.x / a.p.n_seqs * W::KEYS;
+  const int b = blockIdx.x % a.p.n_seqs;
   const SeqRange s = seq_range(a.p, b);
+  const int kb = key_range(a, s, 0, 1).lo + blockIdx.x / a.p.n_seqs * W::KEYS;    // from the first key that a window leaves
   if (kb >= s.len || s.q == 0) return;
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)b * slots : nullptr;
@@ -1047,16 +1076,17 @@ __global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, 
   }
 }
 
-__global__ __launch_bounds__(256) void attention_paged_add_weights_kernel(PagedArgs p, const float* __restrict__ sums, int n,
-                                                                          int ld, float* __restrict__ weight) {
-  const int b = blockIdx.y, key = blockIdx.x * 256 + threadIdx.x;
-  const SeqRange s = seq_range(p, b);
+__global__ __launch_bounds__(256) void attention_paged_add_weights_kernel(AttnArgs a, const float* __restrict__ sums, int n,
+                                                                          float* __restrict__ weight) {
+  const int b = blockIdx.y;
+  const SeqRange s = seq_range(a.p, b);
+  const int key = key_range(a, s, 0, 1).lo + blockIdx.x * 256 + threadIdx.x;
   if (key >= s.len || s.q == 0) return;
-  const float* src = sums + (size_t)b * n * ld + key;
+  const float* src = sums + (size_t)b * n * a.ld_scores + key;
   float v = 0.f;
 #pragma unroll 8
-  for (int h = 0; h < n; ++h) v += src[(size_t)h * ld];
-  weight[((size_t)b * p.max_pages << p.page_shift) + key] += v;
+  for (int h = 0; h < n; ++h) v += src[(size_t)h * a.ld_scores];
+  weight[((size_t)b * a.p.max_pages << a.p.page_shift) + key] += v;
 }
 
 // The same from the scores that the attention itself left, for calls of up to 16 rows a head.  A workgroup takes 256 keys, four a
@@ -1072,7 +1102,7 @@ __global__ __launch_bounds__(256) void attention_paged_score_weights_kernel(Attn
   const int rows = s.q * a.G, n = a.p.n_kv * rows;
   if (rows == 0) return;
   const KeyRange kr = key_range(a, s, 0, 16);                    // lo is a multiple of 64
-  const int n_pieces = div_by(kr.hi - kr.lo + a.split - 1, a.split_magic);
+  const int n_pieces = pieces_of(a, kr);
   if ((int)blockIdx.x >= n_kb) {
     const int r = ((int)blockIdx.x - n_kb) * 4 + wave, h = r / rows, m = r - h * rows;
     const int i = token_of(a, m);
@@ -1165,12 +1195,13 @@ Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G,
     int least = p.tile || (p.rowsplit && head_dim == 64) ? 256 : 128;        // keys of a piece
     if (p.tile || p.rowsplit) {
       // bf16: as many as are resident, four a compute unit, of 128-wide heads two.  Where there is a workgroup a compute unit anyway,
-      // only in pieces long enough to pay for being joined (12 chunks of up to 333 tokens over 3000, 12 heads: 59 us whole, 40 + 5 in
-      // three; 5 prompts of 1024: 24 whole, 25 + 10 in two).
-      // fp32: twice as many, a step is long there (8 chunks of up to 256 tokens over 1024, 12 heads of 64: 66 us whole, 45 + 5 in
+      // only in pieces that are long on average (the rows of a whole prompt see half of it) and pay for being joined: 12 chunks of up
+      // to 333 tokens over 3000, 12 heads, 55 us whole, 34 + 5 in two; in a window of 1024, 30 and 22 + 5; 5 prompts of
+      // 1024: 24 whole, 24 + 7 in two.
+      // fp32: twice as many, a step is long there (8 chunks of up to 256 tokens over 1024, 12 heads of 64: 66 us whole, 38 + 5 in
       // pieces; 4 of them with heads of 128: 68 + 5.5 us in pieces of 256 keys, 58 + 7 of 128).
       want = (p.rowsplit ? 2048 : head_dim == 128 ? 512 : 1024) / units;
-      if (p.tile && units >= 256) least = 768;
+      if (p.tile && units >= 256) want = std::min<int64_t>(want, (len < max_len ? len : len - max_new / 2) / 512);
     } else {
       // Eight steps of a workgroup take as long as the second launch that joins pieces (one sequence of 777 tokens, 12 heads of 64:
       // 8.0 us in one piece, 4.4 + 4.0 in seven).  From two workgroups a compute unit on, cutting gains less than that launch
@@ -1234,7 +1265,8 @@ template <typename T, int DH, int FEAT>
 llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, float* sums, float* weight, hipStream_t st) {
   const bool fast_cap = p.tile && FEAT == 1 && !a.slopes && at->softcap <= (weight ? 64.f : 1024.f);
   set_scores(a, at, fast_cap);
-  const dim3 grid((unsigned)a.p.n_kv, (unsigned)p.n_split, (unsigned)p.blocks);
+  const int64_t items = p.blocks * p.n_split;
+  const dim3 grid((unsigned)a.p.n_kv, (unsigned)std::min<int64_t>(items, 32768), (unsigned)((items + 32767) / 32768));
   {
     ProfScope ps_("attention_paged_kernel", st);
     if (!p.tile && !p.rowsplit) {
@@ -1267,15 +1299,17 @@ llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, fl
     LLMC_LAUNCH_CHECK("attention_paged_score_weights");
   } else if (weight) {
     constexpr int keys = WeightCfg<T, DH>::KEYS;
+    // keys that the new tokens of a sequence see, at most; the first one rounded down to a multiple of 64
+    const int seen = a.window > 0 && !a.pos ? (int)std::min<int64_t>(a.p.max_len, (int64_t)a.window + a.p.max_new + 62) : a.p.max_len;
     set_scores(a, at, false);
     { ProfScope ps_("attention_paged_weight_kernel", st);
-      const dim3 wg((unsigned)((a.p.max_len + keys - 1) / keys * a.p.n_seqs), (unsigned)a.p.n_kv, (unsigned)p.shares);
+      const dim3 wg((unsigned)((seen + keys - 1) / keys * a.p.n_seqs), (unsigned)a.p.n_kv, (unsigned)p.shares);
       if (FEAT == 1 && !a.slopes) LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, 0>), wg, dim3(64), 0, st, a, sums);
       else LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), wg, dim3(64), 0, st, a, sums); }
     LLMC_LAUNCH_CHECK("attention_paged_weight");
     { ProfScope ps_("attention_paged_add_weights_kernel", st);
-      LLMC_KERNEL_GGL(attention_paged_add_weights_kernel, dim3((a.p.max_len + 255) / 256, a.p.n_seqs), dim3(256), 0, st, a.p,
-                      sums, a.p.n_kv * p.shares, a.ld_scores, weight); }
+      LLMC_KERNEL_GGL(attention_paged_add_weights_kernel, dim3((seen + 255) / 256, a.p.n_seqs), dim3(256), 0, st, a, sums,
+                      a.p.n_kv * p.shares, weight); }
     LLMC_LAUNCH_CHECK("attention_paged_add_weights");
   }
   return LLMC_OK;
@@ -1292,7 +1326,7 @@ size_t attention_paged_ws_bytes(int dtype, int head_dim, int n_kv, int H, int n_
 bool attention_paged_grid_ok(int dtype, int head_dim, int n_kv, int H, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
   const Plan p = make_plan(dtype, head_dim, n_rows, n_seqs, n_kv, H / n_kv, max_new, max_len, max_len);
   const int64_t most = 0x7FFFFFFF;
-  return p.blocks <= 65535 && p.n_split <= 65535 && (int64_t)n_rows * H <= most && p.blocks * n_kv <= most / p.n_split &&
+  return p.blocks <= most / n_kv / p.n_split && (int64_t)n_rows * H <= most &&
          (!weights || (int64_t)((max_len + 15) / 16) <= most / n_seqs);
 }
 
@@ -1313,7 +1347,7 @@ llmc_status_t launch_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_bat
   a.softcap = at->softcap;
   a.window = at->window; a.slopes = at->d_slopes;
   a.pos = (at->window > 0 || at->d_slopes) ? bt->d_pos : nullptr;
-  a.split = p.split; a.n_split = p.n_split;
+  a.split = p.split; a.n_split = p.n_split; a.blocks = (int)p.blocks;
   char* w = (char*)ws;
   a.part_o = (float*)(w + l.part_o); a.part_ml = (float2*)(w + l.part_ml);
   a.lse = weights ? (float*)(w + l.lse) : nullptr;
