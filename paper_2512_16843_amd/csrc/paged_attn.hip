@@ -563,10 +563,14 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   }
 }
 
-// ---- the pieces of a long axis joined: a wavefront a (row, head) -------------------------------------------------------
+// ---- the pieces of a long axis joined: a workgroup a (row, head), its wavefronts a quarter of the pieces each -------------
 template <typename T, int DH>
 __device__ __forceinline__ void join_pieces(const AttnArgs& a, int row, int head, int n) {
-  const int lane = threadIdx.x & 63;
+  // 16 bytes a lane: a wavefront takes 256 / DH pieces a step
+  constexpr int L = DH / 4, STEP = 64 / L;
+  __shared__ float4 part_y[3][L];
+  __shared__ float part_l[3];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane / L, dim = lane % L * 4;
   const size_t rh = (size_t)row * a.H + head;
   const float2* ml = a.part_ml + rh * a.n_split;
   const float* po = a.part_o + rh * a.n_split * DH;
@@ -575,12 +579,9 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, int row, int head
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const float top_use = top == -INFINITY ? 0.f : top;
-  // 16 bytes a lane: the wavefront takes 256 / DH pieces a step
-  constexpr int L = DH / 4, STEP = 64 / L;
-  const int sub = lane / L, dim = lane % L * 4;
   float l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int j = sub; j < n; j += STEP) {
+  for (int j = wave * STEP + sub; j < n; j += 4 * STEP) {
     const float2 v = ml[j];
     const float4 p = *reinterpret_cast<const float4*>(po + (size_t)j * DH + dim);
     const float f = __builtin_amdgcn_exp2f(v.x - top_use);
@@ -593,19 +594,30 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, int row, int head
 #pragma unroll
     for (int t = 0; t < 4; ++t) y[t] += __shfl_xor(y[t], o, 64);
   }
+  if (wave > 0 && sub == 0) {
+    part_y[wave - 1][lane] = make_float4(y[0], y[1], y[2], y[3]);
+    if (lane == 0) part_l[wave - 1] = l;
+  }
+  __syncthreads();
+  if (wave > 0 || sub > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const float4 v = part_y[w][lane];
+    l += part_l[w];
+    y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
+  }
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
 #pragma unroll
   for (int t = 0; t < 4; ++t) y[t] *= inv;
-  if (sub == 0) store_vec<T, 4>((T*)a.out + (size_t)row * a.ld_out + head * DH + dim, y);
+  store_vec<T, 4>((T*)a.out + (size_t)row * a.ld_out + head * DH + dim, y);
   if (a.lse && lane == 0) a.lse[rh] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
 }
 
-// one token of each sequence, or few: a wavefront a (row, head)
+// one token of each sequence, or few: grid (heads, rows)
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void attention_paged_join_kernel(AttnArgs a) {
-  const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (rh >= (int64_t)a.p.n_rows * a.H) return;
-  const int row = (int)(rh / a.H), head = (int)(rh % a.H);
+  const int head = blockIdx.x, row = blockIdx.y + blockIdx.z * gridDim.y;
+  if (row >= a.p.n_rows) return;
   const int b = seq_of_row(a.p, row);
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
@@ -1104,7 +1116,7 @@ __global__ __launch_bounds__(256) void attention_paged_score_weights_kernel(Attn
   const KeyRange kr = key_range(a, s, 0, 16);                    // lo is a multiple of 64
   const int n_pieces = pieces_of(a, kr);
   if ((int)blockIdx.x >= n_kb) {
-    const int r = ((int)blockIdx.x - n_kb) * 4 + wave, h = r / rows, m = r - h * rows;
+    const int r = (int)blockIdx.x - n_kb, h = r / rows, m = r - h * rows;
     const int i = token_of(a, m);
     if (r < n && n_pieces > 1) join_pieces<T, DH>(a, s.first + i, h * a.G + m - i * a.G, n_pieces);
     return;
@@ -1208,8 +1220,10 @@ Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G,
       // (64 sequences of up to 2048: 42 and 47 + 4); below, pieces even out ragged lengths (6 of up to 32768, 8 heads of 128: 1024
       // workgroups 106 + 4.5 us, 2048 92 + 7, 4096 93 + 10).  Down to a step of a workgroup, two in fp32 (8 of up to 1000 in fp32, 12
       // heads of 64, biased: 13.4 us in pieces of 256 keys, 10.5 of 128; 8 of up to 1200 in bf16: 7.7 and 6.8).
+      // More than 128 pieces of one axis only where there would be less than two workgroups a compute unit (one of 100000 tokens, 8 heads of
+      // 128: 78 + 6.6 us in 256, 76 + 5 in 128).
       const int steps8 = 8 * 4 * (dtype == LLMC_BF16 ? 32 : 16);
-      want = len <= steps8 || units >= 512 ? 1 : 2048 / units;
+      want = len <= steps8 || units >= 512 ? 1 : std::min<int64_t>(2048 / units, std::max<int64_t>(128, 512 / units));
     }
     want = std::max<int64_t>(1, std::min<int64_t>({want, most, len / least}));
     p.split = (int)std::max<int64_t>(least, align_up((size_t)((len + want - 1) / want), 128));
@@ -1284,7 +1298,7 @@ llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, fl
   if (p.n_split > 1 && !a.scores) {
     ProfScope ps_("attention_paged_join_kernel", st);
     constexpr int heads = 256 / DH;
-    const dim3 one((unsigned)(((int64_t)a.p.n_rows * a.H + 3) / 4));
+    const dim3 one((unsigned)a.H, (unsigned)std::min(a.p.n_rows, 32768), (unsigned)((a.p.n_rows + 32767) / 32768));
     const dim3 many((unsigned)(((int64_t)a.p.n_rows * ((a.H + heads - 1) / heads) + 3) / 4));
     if (p.rows == 128) LLMC_KERNEL_GGL((attention_paged_join_rows_kernel<T, DH, 128>), many, dim3(256), 0, st, a);
     else if (p.rows == 64) LLMC_KERNEL_GGL((attention_paged_join_rows_kernel<T, DH, 64>), many, dim3(256), 0, st, a);
@@ -1293,7 +1307,7 @@ llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, fl
   }
   if (weight && a.scores) {
     { ProfScope ps_("attention_paged_weight_kernel", st);
-      const int n_kb = (a.p.max_len + 255) / 256, n_join = p.n_split > 1 ? (p.join_rows * a.p.n_kv + 3) / 4 : 0;
+      const int n_kb = (a.p.max_len + 255) / 256, n_join = p.n_split > 1 ? p.join_rows * a.p.n_kv : 0;
       LLMC_KERNEL_GGL((attention_paged_score_weights_kernel<T, DH>), dim3(n_kb + n_join, a.p.n_seqs), dim3(256), 0, st, a, weight,
                       n_kb); }
     LLMC_LAUNCH_CHECK("attention_paged_score_weights");
