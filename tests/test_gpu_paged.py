@@ -250,6 +250,16 @@ def test_single_tokens_of_many_heads_on_one_key(L, dtype, heads, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,decode", [(1, True), (1, False), (5, False)])
+def test_more_sequences_than_lanes_in_pieces(L, dtype, new, decode):
+    """70 sequences that share one key/value head, two of them long: their axis is cut."""
+    lens = [40 + 3 * i for i in range(70)]
+    lens[7], lens[66] = 3000, 1999
+    c = Case(L, dtype, 4, 1, 64, 16, lens, [new] * 70, seed=15, weights=True)
+    c.check(c.gpu(decode=decode))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("news", [[1, 1, 1], [40, 3, 100]])
 def test_a_pool_beyond_32_bits(L, dtype, news):
     """The same pages at the end of a pool of more than 2^32 elements, and at its start: the same bits."""
