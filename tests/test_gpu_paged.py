@@ -567,3 +567,72 @@ def test_pages_outside_the_pool_are_no_pages(L):
     L.llmc_kv_append(q.cuda(), q.cuda(), kg, vg, bad.cuda(), i32([20, 40]), pos=pos, weight=w)
     torch.cuda.synchronize()
     assert torch.equal(kg.cpu(), k) and torch.equal(vg.cpu(), v)
+
+
+MIXED = [                                                # (dtype, heads, kv, dh, page, lens, news, options)
+    ("bf16", 4, 2, 64, 16, [900, 33, 200], [200, 33, 7], dict(window=150, weights=True)),
+    ("f32", 4, 4, 64, 32, [600, 5], [100, 1], dict(slopes=True, weights=True)),
+    ("bf16", 8, 2, 128, 64, [3000, 1, 700], [1, 1, 1], dict(weights=True)),
+]
+
+
+def test_calls_on_two_streams_at_once(L):
+    """Calls of different shapes on two streams, each with its own workspace, in flight together: the bits of calls alone."""
+    cases = [Case(L, *m[:7], seed=20 + i, **m[7]) for i, m in enumerate(MIXED)]
+    alone = [(c.gpu(), c.w_gpu.cpu()) for c in cases]
+    args = []
+    for c in cases:
+        q, kp, tab = c.q.cuda(), c.k.cuda(), c.table.cuda()
+        n = L.llmc_attention_paged_workspace_bytes(q, kp, tab, max_new=c.max_new, max_len=c.max_len, weights=True)
+        args.append((q, kp, c.v.cuda(), tab, i32(c.lens), n, i32(c.starts), None if c.slopes is None else c.slopes.cuda()))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    runs = []
+    torch.cuda.synchronize()
+    for rep in range(6):
+        for i, (c, a) in enumerate(zip(cases, args)):
+            q, kp, vp, tab, length, n, start, slopes = a
+            with torch.cuda.stream(streams[(rep + i) & 1]):
+                out, w = torch.zeros_like(q), c.weight.cuda()
+                ws = torch.empty((n,), dtype=torch.uint8, device="cuda")
+                L.llmc_attention_paged(q, kp, vp, tab, length, out, ws, new_start=start, max_new=c.max_new, max_len=c.max_len,
+                                       weight=w, slopes=slopes, **c.opt)
+                runs.append((i, out, w, ws))
+    torch.cuda.synchronize()
+    for i, out, w, _ in runs:
+        assert torch.equal(out.cpu(), alone[i][0]) and torch.equal(w.cpu(), alone[i][1]), i
+
+
+def test_recorded_calls_share_a_workspace(L):
+    """Two graphs recorded with one workspace, replayed in turn with an eager call in it between: no call needs what another left."""
+    cases = [Case(L, *m[:7], seed=20 + i, **m[7]) for i, m in enumerate(MIXED)]
+    alone = [(c.gpu(), c.w_gpu.cpu()) for c in cases]
+    args, need = [], 0
+    for c in cases:
+        q, kp, tab = c.q.cuda(), c.k.cuda(), c.table.cuda()
+        need = max(need, L.llmc_attention_paged_workspace_bytes(q, kp, tab, max_new=c.max_new, max_len=c.max_len, weights=True))
+        args.append([q, kp, c.v.cuda(), tab, i32(c.lens), torch.zeros_like(q)])
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    extra = [(i32(c.starts), c.weight.cuda(), None if c.slopes is None else c.slopes.cuda()) for c in cases]
+
+    def call(i):
+        c, (start, w, slopes) = cases[i], extra[i]
+        L.llmc_attention_paged(*args[i], ws, new_start=start, max_new=c.max_new, max_len=c.max_len, weight=w, slopes=slopes, **c.opt)
+
+    graphs = []
+    for i in (0, 1):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(i)
+        graphs.append(g)
+    for rep in range(4):
+        for i in range(3):
+            extra[i][1].copy_(cases[i].weight)
+            args[i][5].fill_(7.0)
+            if i < 2:
+                graphs[i].replay()
+            else:
+                call(i)
+        torch.cuda.synchronize()
+        for i in range(3):
+            assert torch.equal(args[i][5].cpu(), alone[i][0]) and torch.equal(extra[i][1].cpu(), alone[i][1]), (rep, i)
+        ws.fill_(rep)
