@@ -8,6 +8,7 @@ from __future__ import annotations
 
 from typing import List, Optional
 
+import numpy as np
 import torch
 
 from . import llmc
@@ -203,6 +204,7 @@ class PagedStack:
         self.weight = [torch.zeros(slots, dtype=torch.float32, device=device) for _ in self.layers] if budget else None
         self.free = list(range(n_pages - 1, -1, -1))
         self.pages: List[List[int]] = [[] for _ in range(n_seqs)]
+        self.table = np.full((n_seqs, self.max_pages), -1, dtype=np.int32)      # the same as the device sees it
         self.lengths = [0] * n_seqs           # tokens in the cache
         self.next_pos = [0] * n_seqs          # tokens ever seen: the position of the next one
         self.workspace = torch.empty((0,), dtype=torch.uint8, device=device)
@@ -223,17 +225,20 @@ class PagedStack:
         want = [(n + self.page - 1) // self.page - len(p) for n, p in zip(lens, self.pages)]
         if sum(w for w in want if w > 0) > len(self.free):
             raise ValueError("no pages left")
-        for p, w in zip(self.pages, want):
-            p.extend(self.free.pop() for _ in range(w))
+        for b, (p, w) in enumerate(zip(self.pages, want)):
+            if w > 0:
+                got = [self.free.pop() for _ in range(w)]
+                self.table[b, len(p):len(p) + w] = got
+                p.extend(got)
         starts = [0]
         for q in new:
             starts.append(starts[-1] + q)
         # one copy brings the tables of the call: page table, lengths, starts, positions of the new tokens, budgets
-        host = [p[c] if c < len(p) else -1 for p in self.pages for c in range(self.max_pages)] + lens + starts
+        host = [self.table.ravel(), lens, starts]
         keep = [min(n, self.budget) for n in lens]
         if self.budget:
-            host += [self.next_pos[b] + i for b in range(B) for i in range(new[b])] + keep
-        flat = torch.tensor(host, dtype=torch.int32).pin_memory().to(self.device, non_blocking=True)
+            host += [np.arange(n, n + q) for n, q in zip(self.next_pos, new)] + [keep]
+        flat = torch.from_numpy(np.concatenate(host).astype(np.int32)).pin_memory().to(self.device, non_blocking=True)
         sizes = [B * self.max_pages, B, B + 1] + ([starts[-1], B] if self.budget else [])
         parts = flat.split(sizes)
         table, length, start = parts[0].view(B, self.max_pages), parts[1], parts[2]
@@ -262,12 +267,18 @@ class PagedStack:
             x = y
         self.lengths = keep if self.budget else lens
         self.next_pos = [n + q for n, q in zip(self.next_pos, new)]
-        for b, p in enumerate(self.pages):
-            while len(p) > (self.lengths[b] + self.page - 1) // self.page:
-                self.free.append(p.pop())
+        if cut:
+            for b, n in enumerate(self.lengths):
+                self._free_pages(b, (n + self.page - 1) // self.page)
         return out
+
+    def _free_pages(self, seq: int, left: int) -> None:
+        p = self.pages[seq]
+        self.free.extend(p[left:])
+        self.table[seq, left:len(p)] = -1
+        del p[left:]
 
     def release(self, seq: int) -> None:
         """Forgets sequence ``seq``; its pages are free for the next ``extend`` (on the same stream)."""
-        self.free.extend(self.pages[seq])
-        self.pages[seq], self.lengths[seq], self.next_pos[seq] = [], 0, 0
+        self._free_pages(seq, 0)
+        self.lengths[seq], self.next_pos[seq] = 0, 0
