@@ -606,8 +606,10 @@ typedef struct {
  * Attention of the new tokens (stored beforehand) over their sequences' caches: d_out[r] [n_heads, head_dim] = sum_j p_j v_j,
  * p = softmax of x over the slots that the token sees; zeros where it sees none.  d_q and d_out: rows ld_q and ld_out elements
  * apart (multiples of 16 bytes), element type of the cache; d_out must not overlap d_q or the pages.
- * Softmax statistics, sums and accumulated weights are fp32 in a fixed order (no atomics); with bf16 elements the weights of
- * the value product are rounded to bf16.  What slots beyond a sequence's length hold does not matter.
+ * Softmax statistics, sums and accumulated weights are fp32 in a fixed order (no atomics).  With bf16 elements the weights of the
+ * value product are rounded: up to 16 rows a key/value head (new tokens times query heads of a group) to 16 bits, more to 8 (bf16).
+ * Of more rows the normaliser is the sum of the rounded weights, with accumulate that of the weights as they are: the outputs may
+ * then differ in their last bits.  What slots beyond a sequence's length hold does not matter.
  * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.  (With accumulate and
  * up to 16 rows a key/value head -- new tokens times query heads of a group -- it holds a score a query head and slot.)
  * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite or so far apart that
