@@ -626,7 +626,8 @@ size_t llmc_attention_paged_workspace_bytes(const llmc_kv_desc_t* kv, const llmc
  * Keep a cache within a budget, by the rule of Section IV-D turned to tokens (what has been used least goes): of every sequence
  * with d_length[b] > d_keep[b], the tokens that come first by ascending (protected, weight, position, slot) are evicted until
  * d_keep[b] are left.  Protected are the positions below n_sink and the n_recent highest position numbers of the sequence
- * (they go last).  A NaN weight ranks above every number.  The kept tokens of slots d_keep[b] and up then move into the slots
+ * (they go last).  A NaN weight ranks above every number.  Slots whose page is no page are apart from this: below d_keep[b]
+ * they stay as they are (and count), from d_keep[b] on their tokens go, and the rule holds among the others.  The kept tokens of slots d_keep[b] and up then move into the slots
  * that fell free below, the i-th of them into the i-th of those, with their position and weight; slots from the new length on
  * keep what they held.
  *   batch: d_pos and d_weight are needed; d_new_start, n_rows and max_new are ignored.  Every page of a sequence that is cut

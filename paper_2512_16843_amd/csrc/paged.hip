@@ -58,6 +58,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // their number is at most the number of evicted tokens (closing the gaps in order would move nearly every token for each
 // one that goes).
 //
+// A slot whose page is none can neither give its token away nor take one: below k it stays as it is, from k on its token goes,
+// and the others are chosen among the slots that have pages.  Holes and movers are then as many as each other, all in pages.
+//
 // The choice: one workgroup per sequence.  A token's key is 64 bits (protected flag, weight, position); the (n - k)-th smallest is
 // narrowed by digits of 11 bits, most significant first, a histogram in LDS a digit, until at most 64 keys share the digits
 // so far (two digits, as weights go); a wavefront then ranks those by key and slot.  Holes and movers are numbered by counts
@@ -79,9 +82,11 @@ struct EvictArgs {
   int32_t max_moves;
 };
 
-// order of a weight: ascending, -0 as +0, NaN above every number (a token whose weight cannot be told is kept)
+// order of a weight: ascending, -0 as +0, NaN above every number (a token whose weight cannot be told is kept).  The lowest and
+// the highest value are no weight's: evict_key's ends of the order are left to slots without a page.
+constexpr uint64_t kGoesFirst = 0, kGoesLast = ~0ull;
 __device__ __forceinline__ uint32_t weight_order(float w) {
-  if (w != w) return 0xFFFFFFFFu;
+  if (w != w) return 0xFFFFFFFEu;
   const uint32_t u = __float_as_uint(w + 0.f);
   return (u >> 31) ? ~u : (u | 0x80000000u);
 }
@@ -98,7 +103,8 @@ __global__ __launch_bounds__(kSelThreads) void kv_evict_select_kernel(EvictArgs 
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t totals[kSelWaves];
   __shared__ uint32_t sh_digit, sh_before, sh_count, sh_n;
-  __shared__ int sh_last[kSelWaves], sh_slot;
+  __shared__ int2 sh_last[kSelWaves];                            // a wavefront's highest position, and whether it found a bad page
+  __shared__ int sh_slot;
   __shared__ uint64_t sh_key;
   __shared__ uint64_t cand_key[64];
   __shared__ int cand_slot[64];
@@ -116,6 +122,11 @@ __global__ __launch_bounds__(kSelThreads) void kv_evict_select_kernel(EvictArgs 
     }
     return;
   }
+  const int32_t* table = a.table + (size_t)b * a.max_pages;
+  const auto page = [&](int slot) {
+    const int p = table[slot >> a.page_shift];
+    return (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
+  };
   const int rounds = E ? E : (n + kSelThreads - 1) / kSelThreads;
   uint64_t key[E ? E : 1];
   int last = INT32_MIN;
@@ -135,22 +146,30 @@ __global__ __launch_bounds__(kSelThreads) void kv_evict_select_kernel(EvictArgs 
   } else {
     for (int j = tid; j < n; j += kSelThreads) last = max(last, pos[j]);
   }
+  bool some_bad = false;                                         // is there a slot without a page?
+  for (int i = tid; i <= (n - 1) >> a.page_shift; i += kSelThreads) some_bad |= (uint32_t)table[i] >= (uint32_t)a.n_pages;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) last = max(last, __shfl_xor(last, o, 64));
-  if (lane == 0) sh_last[wave] = last;
+  const bool wave_bad = __ballot(some_bad) != 0;
+  if (lane == 0) sh_last[wave] = make_int2(last, wave_bad);
   for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
   if (tid == 0) sh_n = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) last = max(last, sh_last[w]);
+  for (int w = 0; w < kSelWaves; ++w) {
+    last = max(last, sh_last[w].x);
+    some_bad |= sh_last[w].y != 0;
+  }
+  const auto order = [&](float w, int p, int j) {
+    if (some_bad && page(j) < 0) return j < keep ? kGoesLast : kGoesFirst;
+    return evict_key(w, p, last, a.sink, a.recent);
+  };
   if (E) {
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      key[e] = evict_key(__uint_as_float((uint32_t)(key[e] >> 32)), (int)(uint32_t)key[e], last, a.sink, a.recent);
+      key[e] = order(__uint_as_float((uint32_t)(key[e] >> 32)), (int)(uint32_t)key[e], min(e * kSelThreads + tid, n - 1));
   }
-  const auto key_at = [&](int e, int j) {
-    return E ? key[E ? e : 0] : evict_key(weight[j], pos[j], last, a.sink, a.recent);
-  };
+  const auto key_at = [&](int e, int j) { return E ? key[E ? e : 0] : order(weight[j], pos[j], j); };
   // digits of the key, then (equal keys only) of the slot, until at most 64 tokens are left to choose among
   uint64_t prefix = 0;
   uint32_t slot_prefix = 0, need = n - keep, count = n;
@@ -226,11 +245,6 @@ __global__ __launch_bounds__(kSelThreads) void kv_evict_select_kernel(EvictArgs 
   const uint64_t top = sh_key;
   const int top_slot = sh_slot;
   int4* moves = a.moves + (size_t)b * a.max_moves;
-  const int32_t* table = a.table + (size_t)b * a.max_pages;
-  const auto page = [&](int slot) {
-    const int p = table[slot >> a.page_shift];
-    return (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
-  };
   // 0: stays where it is, 1: a hole, 2: moves
   const auto part_of = [&](uint64_t k, int j) {
     const bool gone = k < top || (k == top && j <= top_slot);
@@ -324,7 +338,6 @@ __global__ __launch_bounds__(256) void kv_evict_move_kernel(EvictArgs a, uint4* 
       a.pos[row + m.z] = a.pos[row + m.x];
       a.weight[row + m.z] = a.weight[row + m.x];
     }
-    if (m.y < 0 || m.w < 0) continue;
     const size_t src = (((((size_t)m.y * a.n_kv + h) << a.page_shift) + (m.x & mask)) << vec_shift) + c;
     const size_t dst = (((((size_t)m.w * a.n_kv + h) << a.page_shift) + (m.z & mask)) << vec_shift) + c;
     const uint4 x = k[src], y = v[src];

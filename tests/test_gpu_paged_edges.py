@@ -29,3 +29,65 @@ def test_few_rows_are_weighted_to_sixteen_bits(L, heads, kv, dh, lens, news, opt
     tol = tol + size * (2.0 ** -16 - 2.0 ** -8 + (max(lens) + 64) * 2.0 ** -24)
     over = ((got.double() - want).abs() - tol).max()
     assert over <= 0, over
+
+
+def evicted(L, lens, keep, sink, recent, table, k, v, pos, weight):
+    """(k, v, pos, weight, new lengths) after the call, on the CPU."""
+    kg, vg, tg, pg, wg = (t.cuda() for t in (k, v, table, pos, weight))
+    out = torch.full((len(lens),), -9, dtype=torch.int32, device="cuda")
+    ws = torch.full((L.llmc_kv_evict_workspace_bytes(tg, max(lens)),), 255, dtype=torch.uint8, device="cuda")
+    L.llmc_kv_evict(kg, vg, tg, i32(lens), pg, wg, i32(keep), out, ws, max_len=max(lens), sink=sink, recent=recent)
+    torch.cuda.synchronize()
+    return kg.cpu(), vg.cpu(), pg.cpu(), wg.cpu(), out.tolist()
+
+
+@pytest.mark.parametrize("lens,keep,sink,recent", [
+    ([100, 60], [70, 33], 4, 8),
+    ([64, 64], [16, 0], 20, 16),                   # more protected tokens than are kept
+    ([3000, 900], [1500, 899], 0, 64),
+    ([5000, 8000], [4000, 100], 16, 0),
+    ([33000, 40], [20000, 20], 0, 0),
+])
+@pytest.mark.parametrize("weights", ["spread", "ends"])
+def test_eviction_leaves_slots_without_a_page_alone(L, lens, keep, sink, recent, weights):
+    """Entries of the table outside the pool, under holes, movers and protected tokens: such slots neither give nor take a token,
+    and what the others hold is chosen among the tokens that have pages."""
+    page, B = 16, len(lens)
+    g = torch.Generator().manual_seed(sum(lens))
+    k, v, table = R.make_cache(g, torch.bfloat16, 2, 64, page, lens, fill=0.25)
+    slots = table.shape[1] * page
+    pos = torch.stack([torch.randperm(2 * slots, generator=g)[:slots] for _ in range(B)]).to(torch.int32)
+    w = torch.exp(2 * torch.randn((B, slots), generator=g))
+    if weights == "ends":                          # the ends of the weights' order, and of the positions'
+        for x, every in ((float("nan"), 3), (float("inf"), 5), (-float("inf"), 4), (0.0, 7)):
+            w[:, ::every] = x
+        pos[:, 1] = 2 ** 31 - 1
+        w[:, 1] = float("nan")
+    for b, n in enumerate(lens):
+        cols = (n + page - 1) // page
+        for i, c in enumerate({0, cols // 2, cols - 1, max(0, keep[b] // page - 1), min(cols - 1, keep[b] // page)}):
+            table[b, c] = (k.shape[0], -7, 2 ** 30)[i % 3]
+    got = evicted(L, lens, keep, sink, recent, table, k, v, pos, w)
+    has = lambda b, j: 0 <= int(table[b, j // page]) < k.shape[0]
+    for b, n in enumerate(lens):
+        m = max(0, min(keep[b], n))
+        on = [j for j in range(n) if has(b, j)]
+        below = sum(j < m for j in on)
+        last = max(pos[b, :n].tolist())
+        p, ww = pos[b].tolist(), w[b].tolist()
+
+        def order(j):
+            x = ww[j]
+            return (p[j] < sink or p[j] > last - recent, (1, 0.0) if x != x else (0, x), p[j], j)
+
+        gone = set(sorted(on, key=order)[:len(on) - below])
+        holes = [j for j in on if j < m and j in gone]
+        movers = [j for j in on if j >= m and j not in gone]
+        assert len(holes) == len(movers)
+        for s, d in zip(movers, holes):
+            ps, pd = int(table[b, s // page]), int(table[b, d // page])
+            k[pd, :, d % page], v[pd, :, d % page] = k[ps, :, s % page], v[ps, :, s % page]
+            pos[b, d], w[b, d] = pos[b, s], w[b, s]
+        assert got[4][b] == m
+    assert torch.equal(got[2], pos) and torch.equal(got[3].view(torch.int32), w.view(torch.int32))
+    assert torch.equal(got[0], k) and torch.equal(got[1], v)
