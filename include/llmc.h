@@ -609,7 +609,8 @@ typedef struct {
  * Softmax statistics, sums and accumulated weights are fp32 in a fixed order (no atomics).  With bf16 elements the weights of the
  * value product are rounded: up to 16 rows a key/value head (new tokens times query heads of a group) to 16 bits, more to 8 (bf16).
  * Of more rows the normaliser is the sum of the rounded weights, with accumulate that of the weights as they are: the outputs may
- * then differ in their last bits.  What slots beyond a sequence's length hold does not matter.
+ * then differ in their last bits.  An infinity or NaN among the values reaches the rows that see it, and no others.  What slots
+ * beyond a sequence's length hold does not matter.
  * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.  (With accumulate and
  * up to 16 rows a key/value head -- new tokens times query heads of a group -- it holds a score a query head and slot.)
  * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite or so far apart that

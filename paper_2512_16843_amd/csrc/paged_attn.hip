@@ -127,6 +127,97 @@ __device__ __forceinline__ void bias_scores(const AttnArgs& a, float (&x)[N], Aw
   }
 }
 
+// a block of rows of a sequence and a piece of its keys
+struct Item { int b, mb, piece; SeqRange s; };      // b < 0: nothing
+
+// ---- rows that may have met a value which they do not see ------------------------------------------------------------------
+// A row's sum is over the keys that it sees, but the value product multiplies every key of a step by a weight, zero where the key is
+// hidden, and zero times an infinity or a NaN is no zero.  Where a row's output is not finite although its normaliser is, the values of
+// the keys that are hidden from some row of the wavefront are looked at; if one of those is not finite, the row is summed again,
+// over what it sees and nothing else.  That is far slower; where all is finite it costs the test of the outputs, which no time
+// shows.  (Infinities in the first token of 16 prompts of 1024 tokens, 12 heads: 5 ms if every row that sees them is summed again.)
+
+// whether a value of a key hidden from some of the rows with slots t_first to t_last is not finite, of keys [lo, hi) and those behind
+// that share their last step
+template <typename T, int DH>
+__device__ __forceinline__ bool hides_odd_values(const AttnArgs& a, const Item& it, int h, int t_first, int t_last, int lo, int hi) {
+  constexpr int PER = DH / Vec16<T>::N;                          // 16-byte vectors of a key
+  hi = min(it.s.len, lo + ((hi - lo + 63) & ~63));
+  const int from = max(lo, t_first + 1);                         // hidden from here on, and up to here
+  const int upto = a.window <= 0 ? lo : a.pos ? hi : (int)min((int64_t)hi, (int64_t)t_last - a.window + 1);
+  const int lane = threadIdx.x & 63;
+  bool any = false;
+#pragma unroll 1
+  for (int key = (upto > lo ? lo : from) + lane / PER; key < hi; key += 64 / PER) {
+    const int page = key < from && key >= upto ? -1 : page_of(a.p, it.b, key);
+    if (page < 0) continue;
+    float v[Vec16<T>::N];
+    Vec16<T>::load((const T*)a.v + ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1))) * DH +
+                       lane % PER * Vec16<T>::N, v);
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N; ++e) any |= !(fabsf(v[e]) < INFINITY);
+  }
+  return __any(any) != 0;
+}
+
+// A row's sum over what it sees: a lane a key for the scores and a lane a dim for the values.  m: the row of the head; ref: what its
+// weights count from; keys: `width` from first, every `step`, up to hi; the DH sums go to part, or times scale to out.  FAST: see cap_scores.
+template <typename T, int DH, bool FAST>
+__device__ __forceinline__ void sum_seen(const AttnArgs& a, const Item& it, int h, int m, float ref, int first, int hi, int step,
+                                         int width, float* part, T* out, float scale) {
+  constexpr int N = DH / 64;
+  const int lane = threadIdx.x & 63, i = token_of(a, m), head = h * a.G + m - i * a.G, t = it.s.len - it.s.q + i;
+  const T* q = (const T*)a.q + (size_t)(it.s.first + i) * a.ld_q + head * DH;
+  const size_t seq = ((size_t)it.b * a.p.max_pages) << a.p.page_shift;
+  const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  const int t_pos = a.pos && t >= 0 ? a.pos[seq + t] : t;
+  const auto place = [&](int page, int key) {
+    return ((((size_t)page * a.p.n_kv + h) << a.p.page_shift) + (key & ((1 << a.p.page_shift) - 1))) * DH;
+  };
+  float o[N] = {};
+  for (int kb = first; kb < hi; kb += step) {
+    const int key = kb + lane;
+    const int page = lane < width && key < hi && key <= t ? page_of(a.p, it.b, key) : -1;
+    int away = 0;
+    float x[1] = {0.f};
+    if (page >= 0) {
+      const T* k = (const T*)a.k + place(page, key);
+#pragma unroll 2
+      for (int d = 0; d < DH; d += Vec16<T>::N) {
+        float qd[Vec16<T>::N], kd[Vec16<T>::N];
+        Vec16<T>::load(q + d, qd);
+        Vec16<T>::load(k + d, kd);
+#pragma unroll
+        for (int e = 0; e < Vec16<T>::N; ++e) x[0] = fmaf(qd[e], kd[e], x[0]);
+      }
+      away = t_pos - (a.pos ? a.pos[seq + key] : key);
+    }
+    if constexpr (FAST) {
+      if (a.softcap > 0.f) cap_scores<true>(a, x);
+      x[0] = fmaf(x[0], a.mul, a.add);
+    } else {
+      bias_scores(a, x, [&](int) { return away; }, slope2);
+    }
+    const float w = __builtin_amdgcn_exp2f(x[0] - ref);
+    const uint64_t seen = __ballot(page >= 0 && !(a.window > 0 && away >= a.window));
+#pragma unroll 2
+    for (int l = 0; l < width; ++l) {                            // the loads of hidden keys are of some page, and not used
+      const float wl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), l));
+      const T* v = (const T*)a.v + place(max(__builtin_amdgcn_readlane(page, l), 0), kb + l);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float ve = Elem<T>::load(v + e * 64 + lane);
+        o[e] = seen >> l & 1 ? fmaf(wl, ve, o[e]) : o[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if (part) part[e * 64 + lane] = o[e];
+    else Elem<T>::store(out + e * 64 + lane, o[e] * scale);
+  }
+}
+
 // ---- pieces of the products for the two element types, 16 query columns a wavefront -----------------------------------
 template <typename T, int DH> struct Frag;
 
@@ -270,7 +361,6 @@ __device__ __forceinline__ int pieces_of(const AttnArgs& a, const KeyRange& kr) 
 // Workgroups are dealt to compute units in turn, whatever they have to do, and idle ones in between leave the work uneven
 // (4 ragged fp32 chunks of 256 tokens over 1024, 12 heads: 33 us with gaps, 28 without; 16 of up to 300 over 4000 in bf16: 60 and
 // 46).  That takes a step a level and lanes for all sequences; larger calls go sequence by sequence from the end, 64 a step.
-struct Item { int b, mb, piece; SeqRange s; };      // b < 0: nothing
 template <int ROWS>
 __device__ __forceinline__ Item item_of(const AttnArgs& a, int idx) {
   const int lane = threadIdx.x & 63;
@@ -508,44 +598,50 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   l_run = sum_over_groups(l_run);
 
   // lane: column c, dims (4 g + r) * NV + t
-  if (ROWSPLIT) {
-    if (!row_there) return;
-    const size_t rh = (size_t)row * a.H + head;
-    if (n_pieces == 1) {
-      const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float y[NV];
-#pragma unroll
-        for (int t = 0; t < NV; ++t) y[t] = o[t][r] * inv;
-        store_vec<T, NV>((T*)a.out + (size_t)row * a.ld_out + head * DH + (4 * g + r) * NV, y);
-      }
-      if (a.lse && g == 0) a.lse[rh] = l_run == 0.f ? INFINITY : m_run + __builtin_amdgcn_logf(l_run);
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float y[NV];
-#pragma unroll
-        for (int t = 0; t < NV; ++t) y[t] = o[t][r];
-        store_vec<float, NV>(a.part_o + (rh * a.n_split + piece) * DH + (4 * g + r) * NV, y);
-      }
-      if (g == 0) a.part_ml[rh * a.n_split + piece] = make_float2(m_run, l_run);
-    }
-    return;
-  }
   const int R = a.join_rows;                                     // at least as many as this block has
   float* sM = rows_lds + NW * R * LDO;
   float* sL = sM + NW * R;
-  if (c < R) {
+  const bool whole = ROWSPLIT && n_pieces == 1;
+  const size_t rh = (size_t)row * a.H + head;
+  const float scale = !whole ? 1.f : l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);
+  float zero = 0.f;                                              // or NaN
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float y[NV];
+  for (int t = 0; t < NV; ++t)
 #pragma unroll
-      for (int t = 0; t < NV; ++t) y[t] = o[t][r];
-      store_vec<float, NV>(&rows_lds[(wave * R + c) * LDO + (4 * g + r) * NV], y);
+    for (int r = 0; r < 4; ++r) zero = fmaf(o[t][r], 0.f, zero);
+  const uint64_t odd = __ballot(zero != 0.f && l_run < INFINITY && row_there);
+  uint32_t again = (uint32_t)(odd | odd >> 16 | odd >> 32 | odd >> 48) & 0xFFFFu;    // a bit a column
+  // (bf16 has two parts of a weight, of any sign or none, and is not right about an infinity that a row does see)
+  if (__builtin_expect(again != 0, 0) && sizeof(T) == 4 &&
+      !hides_odd_values<T, DH>(a, rb, h, t_first, s.len - s.q + min(token_of(a, m0 + 15), s.q - 1), k_lo, k_hi))
+    again = 0;
+  if (ROWSPLIT ? row_there : c < R) {
+    if (!(again >> c & 1)) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float y[NV];
+#pragma unroll
+        for (int t = 0; t < NV; ++t) y[t] = o[t][r] * scale;
+        if (whole) store_vec<T, NV>((T*)a.out + (size_t)row * a.ld_out + head * DH + (4 * g + r) * NV, y);
+        else if (ROWSPLIT) store_vec<float, NV>(a.part_o + (rh * a.n_split + piece) * DH + (4 * g + r) * NV, y);
+        else store_vec<float, NV>(&rows_lds[(wave * R + c) * LDO + (4 * g + r) * NV], y);
+      }
     }
-    if (g == 0) { sM[wave * R + c] = m_run; sL[wave * R + c] = l_run; }
+    if (g == 0) {
+      if (!ROWSPLIT) { sM[wave * R + c] = m_run; sL[wave * R + c] = l_run; }
+      else if (!whole) a.part_ml[rh * a.n_split + piece] = make_float2(m_run, l_run);
+      else if (a.lse) a.lse[rh] = l_run == 0.f ? INFINITY : m_run + __builtin_amdgcn_logf(l_run);
+    }
   }
+  for (; __builtin_expect(again != 0, 0); again &= again - 1) {
+    const int col = __builtin_ctz(again), mr = m0 + col;
+    const auto of_row = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), col)); };
+    const float ref = of_row(m_run), sc = of_row(scale);
+    const int i = token_of(a, mr), r = s.first + i, hd = h * a.G + mr - i * a.G;
+    float* part = whole ? nullptr : ROWSPLIT ? a.part_o + (((size_t)r * a.H + hd) * a.n_split + piece) * DH : rows_lds + (wave * R + col) * LDO;
+    sum_seen<T, DH, false>(a, rb, h, mr, ref, k_first, k_hi, STEP, KEYS, part, (T*)a.out + (size_t)r * a.ld_out + hd * DH, sc);
+  }
+  if (ROWSPLIT) return;
   __syncthreads();
   // joined by a thread a row and dim
   for (int e = threadIdx.x; e < rows * DH; e += NW * 64) {
@@ -958,30 +1054,53 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
       }
     }
   }
-  if (!row_there) return;
   const float l = l_run + __shfl_xor(l_run, 32, 64);
   const size_t rh = (size_t)row * a.H + head;
-  if (n_pieces == 1) {
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-    uint16_t* dst = (uint16_t*)a.out + (size_t)row * a.ld_out + head * DH + half * 4;
+  const bool whole = n_pieces == 1;
+  const float scale = !whole ? 1.f : l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+  float zero = 0.f;                                               // or NaN
 #pragma unroll
-    for (int f = 0; f < NF; ++f)
+  for (int f = 0; f < NF; ++f)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint2 w;
-        w.x = f32x2_to_bf16x2(o[f][4 * j] * inv, o[f][4 * j + 1] * inv);
-        w.y = f32x2_to_bf16x2(o[f][4 * j + 2] * inv, o[f][4 * j + 3] * inv);
-        *reinterpret_cast<uint2*>(dst + f * 32 + 8 * j) = w;
+    for (int r = 0; r < 16; ++r) zero = fmaf(o[f][r], 0.f, zero);
+  const uint64_t odd = __ballot(zero != 0.f && l < INFINITY && row_there);
+  uint32_t again = (uint32_t)(odd | odd >> 32);                   // a bit a row
+  if (__builtin_expect(again != 0, 0) && !hides_odd_values<bf16_t, DH>(a, rb, h, t_first, t_last, k_lo, k_hi)) again = 0;
+  if (row_there) {
+    if (!(again >> (lane & 31) & 1)) {
+      if (whole) {
+        uint16_t* dst = (uint16_t*)a.out + (size_t)row * a.ld_out + head * DH + half * 4;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint2 w;
+            w.x = f32x2_to_bf16x2(o[f][4 * j] * scale, o[f][4 * j + 1] * scale);
+            w.y = f32x2_to_bf16x2(o[f][4 * j + 2] * scale, o[f][4 * j + 3] * scale);
+            *reinterpret_cast<uint2*>(dst + f * 32 + 8 * j) = w;
+          }
+      } else {
+        float* dst = a.part_o + (rh * a.n_split + piece) * DH + half * 4;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<float4*>(dst + f * 32 + 8 * j) =
+                make_float4(o[f][4 * j], o[f][4 * j + 1], o[f][4 * j + 2], o[f][4 * j + 3]);
       }
-    if (a.lse && half == 0) a.lse[rh] = l == 0.f ? INFINITY : m_run + __builtin_amdgcn_logf(l);
-  } else {
-    float* dst = a.part_o + (rh * a.n_split + piece) * DH + half * 4;
-#pragma unroll
-    for (int f = 0; f < NF; ++f)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4*>(dst + f * 32 + 8 * j) = make_float4(o[f][4 * j], o[f][4 * j + 1], o[f][4 * j + 2], o[f][4 * j + 3]);
-    if (half == 0) a.part_ml[rh * a.n_split + piece] = make_float2(m_run, l);
+    }
+    if (half == 0) {
+      if (!whole) a.part_ml[rh * a.n_split + piece] = make_float2(m_run, l);
+      else if (a.lse) a.lse[rh] = l == 0.f ? INFINITY : m_run + __builtin_amdgcn_logf(l);
+    }
+  }
+  for (; __builtin_expect(again != 0, 0); again &= again - 1) {
+    const int col = __builtin_ctz(again), mr = m0 + col;
+    const auto of_row = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), col)); };
+    const float ref = of_row(m_run), sc = of_row(scale);
+    const int i = token_of(a, mr), r = s.first + i, hd = h * a.G + mr - i * a.G;
+    float* part = whole ? nullptr : a.part_o + (((size_t)r * a.H + hd) * a.n_split + piece) * DH;
+    sum_seen<bf16_t, DH, FEAT == 0>(a, rb, h, mr, ref, k_lo, k_hi, 64, 64, part, (bf16_t*)a.out + (size_t)r * a.ld_out + hd * DH, sc);
   }
 }
 

@@ -91,3 +91,73 @@ def test_eviction_leaves_slots_without_a_page_alone(L, lens, keep, sink, recent,
         assert got[4][b] == m
     assert torch.equal(got[2], pos) and torch.equal(got[3].view(torch.int32), w.view(torch.int32))
     assert torch.equal(got[0], k) and torch.equal(got[1], v)
+
+
+def spoil(c, pages, b, slot, head, dims, value):
+    page = c.k.shape[2]
+    pages[int(c.table[b, slot // page]), head, slot % page, dims] = value
+
+
+def who_sees(c, b):
+    """[new tokens, slots] of sequence b: which new token sees which slot."""
+    n, q = c.lens[b], c.starts[b + 1] - c.starts[b]
+    slot = torch.arange(n - q, n)
+    p = c.pos[b, :n].long() if c.pos is not None else torch.arange(n)
+    away = p[slot][:, None] - p[None, :]
+    seen = torch.arange(n)[None, :] <= slot[:, None]
+    return seen & (away < c.opt["window"]) if c.opt["window"] else seen
+
+
+HIDDEN = [
+    # heads, kv, head_dim, lens, news
+    (4, 2, 64, [90, 33, 200], [1, 1, 1]),          # single tokens: hidden by a window alone
+    (4, 2, 64, [90, 12, 8], [4, 8, 2]),            # up to 16 rows a head
+    (3, 3, 64, [200, 300], [200, 70]),
+    (4, 1, 128, [150, 700], [150, 100]),
+    (6, 2, 128, [5000, 100], [30, 40]),            # in pieces
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,dh,lens,news", HIDDEN)
+@pytest.mark.parametrize("opts", [dict(), dict(window=20), dict(window=150, moved=True), dict(softcap=20.0, window=40),
+                                  dict(slopes=True, weights=True), dict(weights=True, window=64)],
+                         ids=lambda o: "-".join(o) or "plain")
+def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(L, dtype, heads, kv, dh, lens, news, opts):
+    """Infinities and NaN among the values of new tokens, and of tokens at the edge of the window: a row that sees none of them is
+    what it is without them; where a row sees them, those dims alone are +infinity, -infinity or NaN.  A weight below 2^-149 is
+    zero in 32 bits, and zero times an infinity NaN: with a slope of 2^-2 the first of 700 tokens has exp(-0.25 * 699) = 2^-252.
+    Below 2^-100 (what follows is 2^-126 and the normaliser, at most 700) either will do."""
+    c = Case(L, dtype, heads, kv, dh, 16, lens, news, seed=41, spread=0.5, **opts)
+    form = dict(pos=c.pos, slopes=c.slopes, **c.opt)
+    want, tol, ws, wt = R.attention(c.q, c.k, c.v, c.table, c.lens, c.starts, **form)
+    up = torch.zeros(want.shape, dtype=torch.bool)
+    down = torch.zeros_like(up)
+    clean, mark = c.v.clone(), torch.nan_to_num(c.v) * 0
+    for b, (n, q) in enumerate(zip(lens, news)):
+        first = max(0, n - q)
+        spots = {0, n - 1, n - q // 2 - 1, first, max(0, first - 19), max(0, first - 20), max(0, first - 63), max(0, first - 64)}
+        for i, slot in enumerate(sorted(spots)):
+            h, dim, value = i % kv, (7 * i + 3) % dh, (float("inf"), -float("inf"), float("nan"))[i % 3]
+            spoil(c, c.v, b, slot, h, dim, value)
+            spoil(c, clean, b, slot, h, dim, 0.0)
+            spoil(c, mark, b, slot, h, dim, 1.0)
+            rows = torch.nonzero(who_sees(c, b)[:, slot])[:, 0] + c.starts[b]
+            for head in range(h * heads // kv, (h + 1) * heads // kv):
+                up[rows, head, dim] |= not value < 0
+                down[rows, head, dim] |= not value > 0
+    want, tol, ws, wt = R.attention(c.q, c.k, clean, c.table, c.lens, c.starts, **form)
+    got = c.gpu(decode=news == [1] * len(news)).double()
+    inf = float("inf")
+    faint = R.attention(c.q, c.k, mark, c.table, c.lens, c.starts, **form)[0] < 2.0 ** -100
+    assert not torch.isfinite(got[(up | down) & faint]).any()
+    got = torch.where((up ^ down) & faint, torch.where(up, inf, -inf).double(), got)
+    assert (got[up & ~down] == inf).all() and (got[down & ~up] == -inf).all() and torch.isnan(got[up & down]).all()
+    rest = ~(up | down)
+    assert torch.isfinite(got[rest]).all()
+    over = ((got - want).abs() - tol)[rest].max()
+    assert over <= 0, over
+    if c.weight is not None:
+        for b, n in enumerate(lens):
+            add = c.w_gpu.cpu()[b].double() - c.weight[b].double()
+            assert ((add[:n] - ws[b]).abs() <= wt[b] + 2.0 ** -23 * (c.weight[b, :n].double() + ws[b])).all()
