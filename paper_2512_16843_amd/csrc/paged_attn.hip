@@ -252,8 +252,8 @@ template <int DH> struct Frag<bf16_t, DH> {
 #pragma unroll
     for (int i = 0; i < NV / 2; ++i) v.w[u * 4 + r][i] = 0;
   }
-  static __device__ __forceinline__ f32x4_t qk(const K& k, int u, const Q& q) {
-    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  static __device__ __forceinline__ f32x4_t qk(const K& k, int u, const Q& q, float from = 0.f) {
+    f32x4_t s = {from, from, from, from};
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v[u][i], q.v[i], s, 0, 0, 0);
     return s;
@@ -310,8 +310,8 @@ template <int DH> struct Frag<float, DH> {
 #pragma unroll
     for (int i = 0; i < NV / 4; ++i) v.w[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  static __device__ __forceinline__ f32x4_t qk(const K& k, int u, const Q& q) {
-    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  static __device__ __forceinline__ f32x4_t qk(const K& k, int u, const Q& q, float from = 0.f) {
+    f32x4_t s = {from, from, from, from};
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
@@ -1185,10 +1185,13 @@ __global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, 
     for (int i = 0; i < RT; ++i) {
       const int first = t_base + token_of(a, min(m0 + 16 * i, rows - 1)), last = t_base + token_of(a, min(m0 + 16 * i + 15, rows - 1));
       const bool edge = first < kb + W::KEYS - 1 || bad || (FEAT != 2 && a.window > 0 && (int64_t)last - kb >= a.window);
-      const float lse = m0 + 16 * i + c < m_hi ? R.lse[i] : INFINITY;       // no such row, or out of the window: weights of zero
+      float lse = m0 + 16 * i + c < m_hi ? R.lse[i] : INFINITY;             // no such row, or out of the window: weights of zero
+      // a row of NaN gives NaN to the keys that it sees, through its products, and nothing to hidden ones (-inf - NaN is NaN too)
+      const float from = lse == lse ? 0.f : lse;
+      lse = lse == lse ? lse : 0.f;
 #pragma unroll
       for (int u = 0; u < TILES; ++u) {
-        const f32x4_t sc = F::qk(fk[u / SUB], u % SUB, R.q[i]);
+        const f32x4_t sc = F::qk(fk[u / SUB], u % SUB, R.q[i], from);
         const int key0 = kb + 16 * u + 4 * g;
         float x[4];
 #pragma unroll

@@ -161,3 +161,39 @@ def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(L, dtype, 
         for b, n in enumerate(lens):
             add = c.w_gpu.cpu()[b].double() - c.weight[b].double()
             assert ((add[:n] - ws[b]).abs() <= wt[b] + 2.0 ** -23 * (c.weight[b, :n].double() + ws[b])).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,dh,lens,news", HIDDEN[:4] + [(4, 1, 64, [900, 40], [400, 40])])
+@pytest.mark.parametrize("opts", [dict(), dict(window=20), dict(window=150, moved=True), dict(softcap=20.0, window=40),
+                                  dict(slopes=True)], ids=lambda o: "-".join(o) or "plain")
+def test_rows_of_nan_give_weight_to_what_they_see_alone(L, dtype, heads, kv, dh, lens, news, opts):
+    """A query that is NaN, a key that is: the rows they concern are NaN, and so is the weight of the slots that these rows see.
+    Every other row, and the weight of every other slot, is what it is without them."""
+    c = Case(L, dtype, heads, kv, dh, 16, lens, news, seed=43, weights=True, **opts)
+    q, k = c.q.clone(), c.k.clone()
+    nan = float("nan")
+    odd = torch.zeros((c.starts[-1], heads), dtype=torch.bool)
+    for b, (n, m) in enumerate(zip(lens, news)):
+        row = c.starts[b] + m // 3
+        if b == 0:
+            c.q[row, heads - 1, 3], q[row, heads - 1] = nan, 0.0
+            odd[row, heads - 1] = True
+        else:
+            slot = max(0, n - m) + m // 3
+            spoil(c, c.k, b, slot, 0, 5, nan)
+            spoil(c, k, b, slot, 0, slice(None), 0.0)
+            rows = torch.nonzero(who_sees(c, b)[:, slot])[:, 0] + c.starts[b]
+            odd[rows, :heads // kv] = True
+    got = c.gpu(decode=news == [1] * len(news)).double()
+    want, tol, ws, wt = R.attention(q, k, c.v, c.table, c.lens, c.starts, pos=c.pos, slopes=c.slopes, **c.opt)
+    assert torch.isnan(got[odd]).all()
+    over = ((got - want).abs() - tol)[~odd].max() if (~odd).any() else 0.0
+    assert over <= 0, over
+    for b, n in enumerate(lens):
+        add = c.w_gpu.cpu()[b].double() - c.weight[b].double()
+        touched = who_sees(c, b)[odd[c.starts[b]:c.starts[b + 1]].any(1)].any(0)
+        assert torch.isnan(add[:n][touched]).all()
+        off = (add[:n] - ws[b]).abs() - wt[b] - 2.0 ** -23 * (c.weight[b, :n].double() + ws[b])
+        assert (off[~touched] <= 0).all(), off[~touched].max()
+        assert (add[n:] == 0).all()
