@@ -54,4 +54,11 @@ __device__ __forceinline__ int page_of(const PagedArgs& a, int b, int slot) {
   return (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
 }
 
+// Workgroups numbered over two dimensions, since no dimension of a launch may have 2^32 threads: their number may be exceeded.
+inline dim3 flat_grid(int64_t workgroups) {
+  const int64_t most = 1 << 22;
+  return dim3((unsigned)(workgroups < most ? workgroups : most), (unsigned)((workgroups + most - 1) / most));
+}
+__device__ __forceinline__ uint32_t flat_block() { return blockIdx.x + blockIdx.y * gridDim.x; }
+
 }  // namespace llmc

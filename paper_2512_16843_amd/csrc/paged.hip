@@ -23,9 +23,10 @@ struct AppendArgs {
 };
 
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
-  const int row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t idx = flat_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (row >= a.p.n_rows) return;
+  if (idx >= (uint32_t)a.p.n_rows) return;
+  const int row = idx;
   const int b = seq_of_row(a.p, row);
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
@@ -370,7 +371,7 @@ llmc_status_t launch_kv_append(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* 
   a.pos_new = pos_new; a.pos = bt->d_pos; a.weight = bt->d_weight;
   a.vec_shift = log2_of(kv->head_dim * e / 16);
   ProfScope ps_("kv_append_kernel", st);
-  LLMC_KERNEL_GGL(kv_append_kernel, dim3((unsigned)((bt->n_rows + 3) / 4)), dim3(256), 0, st, a);
+  LLMC_KERNEL_GGL(kv_append_kernel, flat_grid(((int64_t)bt->n_rows + 3) / 4), dim3(256), 0, st, a);
   LLMC_LAUNCH_CHECK("kv_append");
   return LLMC_OK;
 }

@@ -739,9 +739,9 @@ template <typename T, int DH, int ROWS>
 __global__ __launch_bounds__(256) void attention_paged_join_rows_kernel(AttnArgs a) {
   constexpr int L = DH / 4, HEADS = 64 / L;
   const int lane = threadIdx.x & 63, dim = lane % L * 4;
-  const int idx = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_row = (a.H + HEADS - 1) / HEADS;
+  const uint32_t idx = flat_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_row = (a.H + HEADS - 1) / HEADS;
+  if (idx / per_row >= (uint32_t)a.p.n_rows) return;
   const int row = idx / per_row, head = (idx - row * per_row) * HEADS + lane / L;
-  if (row >= a.p.n_rows) return;
   const int b = seq_of_row(a.p, row);
   if (b < 0) return;
   const SeqRange s = seq_range(a.p, b);
@@ -1118,16 +1118,18 @@ template <typename T, int DH> struct WeightCfg {
 };
 
 template <typename T, int DH, int FEAT>
-__global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, float* __restrict__ sums) {
+__global__ __launch_bounds__(64) void attention_paged_weight_kernel(AttnArgs a, float* __restrict__ sums, int shares) {
   typedef Frag<T, DH> F;
   typedef typename F::E E;
   typedef WeightCfg<T, DH> W;
   constexpr int SUB = F::SUB, TILES = W::TILES, NK = TILES / SUB, RT = W::RT;
   const int lane = threadIdx.x, c = lane & 15, g = lane >> 4;
-  const int h = blockIdx.y, share = blockIdx.z, shares = gridDim.z;
-  const int b = blockIdx.x % a.p.n_seqs;
+  const int h = blockIdx.y;
+  uint32_t share = blockIdx.z, idx = blockIdx.x;
+  for (; share >= (uint32_t)shares; share -= shares) idx += gridDim.x;             // more workgroups than fit one dimension
+  const int b = idx % (uint32_t)a.p.n_seqs;
   const SeqRange s = seq_range(a.p, b);
-  const int kb = key_range(a, s, 0, 1).lo + blockIdx.x / a.p.n_seqs * W::KEYS;    // from the first key that a window leaves
+  const int kb = key_range(a, s, 0, 1).lo + (int)(idx / (uint32_t)a.p.n_seqs) * W::KEYS;      // from the first key that a window leaves
   if (kb >= s.len || s.q == 0) return;
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)b * slots : nullptr;
@@ -1462,7 +1464,7 @@ llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, fl
     ProfScope ps_("attention_paged_join_kernel", st);
     constexpr int heads = 256 / DH;
     const dim3 one((unsigned)a.H, (unsigned)std::min(a.p.n_rows, 32768), (unsigned)((a.p.n_rows + 32767) / 32768));
-    const dim3 many((unsigned)(((int64_t)a.p.n_rows * ((a.H + heads - 1) / heads) + 3) / 4));
+    const dim3 many = flat_grid(((int64_t)a.p.n_rows * ((a.H + heads - 1) / heads) + 3) / 4);
     if (p.rows == 128) LLMC_KERNEL_GGL((attention_paged_join_rows_kernel<T, DH, 128>), many, dim3(256), 0, st, a);
     else if (p.rows == 64) LLMC_KERNEL_GGL((attention_paged_join_rows_kernel<T, DH, 64>), many, dim3(256), 0, st, a);
     else LLMC_KERNEL_GGL((attention_paged_join_kernel<T, DH>), one, dim3(256), 0, st, a);
@@ -1480,9 +1482,10 @@ llmc_status_t launch_t(AttnArgs a, const llmc_attn_desc_t* at, const Plan& p, fl
     const int seen = a.window > 0 && !a.pos ? (int)std::min<int64_t>(a.p.max_len, (int64_t)a.window + a.p.max_new + 62) : a.p.max_len;
     set_scores(a, at, false);
     { ProfScope ps_("attention_paged_weight_kernel", st);
-      const dim3 wg((unsigned)((seen + keys - 1) / keys * a.p.n_seqs), (unsigned)a.p.n_kv, (unsigned)p.shares);
-      if (FEAT == 1 && !a.slopes) LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, 0>), wg, dim3(64), 0, st, a, sums);
-      else LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), wg, dim3(64), 0, st, a, sums); }
+      dim3 wg = flat_grid((int64_t)((seen + keys - 1) / keys) * a.p.n_seqs);
+      wg = dim3(wg.x, (unsigned)a.p.n_kv, wg.y * (unsigned)p.shares);
+      if (FEAT == 1 && !a.slopes) LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, 0>), wg, dim3(64), 0, st, a, sums, p.shares);
+      else LLMC_KERNEL_GGL((attention_paged_weight_kernel<T, DH, FEAT>), wg, dim3(64), 0, st, a, sums, p.shares); }
     LLMC_LAUNCH_CHECK("attention_paged_weight");
     { ProfScope ps_("attention_paged_add_weights_kernel", st);
       LLMC_KERNEL_GGL(attention_paged_add_weights_kernel, dim3((seen + 255) / 256, a.p.n_seqs), dim3(256), 0, st, a, sums,

@@ -197,3 +197,65 @@ def test_rows_of_nan_give_weight_to_what_they_see_alone(L, dtype, heads, kv, dh,
         off = (add[:n] - ws[b]).abs() - wt[b] - 2.0 ** -23 * (c.weight[b, :n].double() + ws[b])
         assert (off[~touched] <= 0).all(), off[~touched].max()
         assert (add[n:] == 0).all()
+
+
+# ---- launches of more workgroups than one dimension takes ------------------------------------------------------------
+
+def test_append_of_rows_beyond_one_dimension(L):
+    """2^26 rows and a few, a wavefront each: 2^32 threads.  All but the last eight belong to no sequence."""
+    n = 2 ** 26 + 5
+    g = torch.Generator().manual_seed(50)
+    k, v, table = R.make_cache(g, torch.bfloat16, 1, 64, 16, [20], fill=0.5)
+    new = torch.zeros((n, 1, 64), dtype=torch.bfloat16, device="cuda")
+    last = torch.randn((8, 1, 64), generator=g).to(torch.bfloat16)
+    new[n - 8:] = last.cuda()
+    kg, vg = k.cuda(), v.cuda()
+    L.llmc_kv_append(new, new, kg, vg, table.cuda(), i32([20]), new_start=i32([n - 8, n]), max_new=8)
+    torch.cuda.synchronize()
+    for got, was in ((kg, k), (vg, v)):
+        assert torch.equal(R.tokens(got.cpu(), table, 0, 20)[:, 12:], last.transpose(0, 1).double())
+        assert torch.equal(R.tokens(got.cpu(), table, 0, 12), R.tokens(was, table, 0, 12))
+
+
+def test_pieces_of_rows_beyond_one_dimension(L):
+    """The last 40 of 2^26 and a few rows attend over a cut axis: the outputs are those of the 40 rows alone."""
+    n = 2 ** 26 + 5
+    c = Case(L, "bf16", 1, 1, 64, 16, [500], [40], seed=51)
+    alone = c.gpu()
+    c.check(alone)
+    q = torch.zeros((n, 1, 64), dtype=torch.bfloat16, device="cuda")
+    q[n - 40:] = c.q.cuda()
+    out = torch.full_like(q, 7.0)
+    kp, vp, tab = c.k.cuda(), c.v.cuda(), c.table.cuda()
+    need = L.llmc_attention_paged_workspace_bytes(q, kp, tab, max_new=40, max_len=512)
+    assert need >= n * 2 * 64 * 4                                  # two pieces, or more
+    ws = torch.empty((need,), dtype=torch.uint8, device="cuda")
+    L.llmc_attention_paged(q, kp, vp, tab, i32([500]), out, ws, new_start=i32([n - 40, n]), max_new=40, max_len=512)
+    torch.cuda.synchronize()
+    got = out[n - 40:].cpu()
+    c.check(got)
+    assert (out[:n - 40] == 7.0).all()
+
+
+def test_weights_of_slots_beyond_one_dimension(L):
+    """65535 sequences of up to 16400 tokens, a wavefront each 16 slots: 2^32 threads.  Three of them have new tokens."""
+    at, B, max_len = [0, 40000, 65534], 65535, 16400
+    c = Case(L, "f32", 1, 1, 128, 16, [30, 16400, 200], [17, 17, 5], seed=52, weights=True)
+    mp = c.table.shape[1]
+    table = torch.full((B, mp), -1, dtype=torch.int32, device="cuda")
+    length, start = torch.zeros((B,), dtype=torch.int32), torch.zeros((B + 1,), dtype=torch.int32)
+    weight = torch.full((B, mp * 16), 3.0, device="cuda")
+    for i, b in enumerate(at):
+        table[b], length[b], weight[b] = c.table[i].cuda(), c.lens[i], c.weight[i].cuda()
+        start[b + 1:] += c.news[i]
+    q, kp = c.q.cuda(), c.k.cuda()
+    out = torch.zeros_like(q)
+    ws = torch.empty((L.llmc_attention_paged_workspace_bytes(q, kp, table, max_new=17, max_len=max_len, weights=True),),
+                     dtype=torch.uint8, device="cuda")
+    L.llmc_attention_paged(q, kp, c.v.cuda(), table, length.cuda(), out, ws, new_start=start.cuda(), max_new=17, max_len=max_len,
+                           weight=weight)
+    torch.cuda.synchronize()
+    c.w_gpu = weight[at]
+    c.check(out.cpu())
+    weight[at] = 3.0
+    assert (weight == 3.0).all()
