@@ -613,8 +613,8 @@ typedef struct {
  * beyond a sequence's length hold does not matter.
  * d_workspace: at least llmc_attention_paged_workspace_bytes(...) bytes for the same sizes, 16-byte aligned.  (With accumulate and
  * up to 16 rows a key/value head -- new tokens times query heads of a group -- it holds a score a query head and slot.)
- * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, scale or softcap not finite or so far apart that
- * scale / softcap overflows), SHAPE (head counts, strides, alignment, bounds), DTYPE, WORKSPACE.
+ * Errors: INVALID_ARG (null, non-positive sizes, accumulate without d_weight, d_out that overlaps, scale or softcap not finite or
+ * so far apart that scale / softcap overflows), SHAPE (head counts, strides, alignment, bounds), DTYPE, WORKSPACE.
  */
 llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const llmc_attn_desc_t* attn,
                                    const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* d_workspace,
@@ -647,7 +647,7 @@ size_t llmc_kv_evict_workspace_bytes(int32_t n_seqs, int32_t max_len);
  * The decoder block (arch 1) on new tokens: x1 = x + MHA(LN1(x)), y = x1 + W2 act(W1 LN2(x1) + b1) + b2 for the n_rows rows of
  * d_h_in [n_rows, d], where the new tokens' keys and values are stored as llmc_kv_append does (positions d_pos_new) and MHA
  * attends as llmc_attention_paged does.  kv: the layer's element type, n_kv_heads = n_heads, head_dim 64; attn->n_heads =
- * layer->n_heads.  d_h_out must not overlap d_h_in; its rows of no sequence are undefined.
+ * layer->n_heads.  d_h_out must not overlap d_h_in or the pages; its rows of no sequence are undefined.
  * d_workspace: at least llmc_layer_paged_workspace_bytes(layer, batch, attn) bytes (sizes only), 256-byte aligned.
  * Errors: as the calls it stands for.
  */

@@ -490,6 +490,31 @@ static llmc_status_t check_attn_values(const llmc_kv_batch_t* bt, const llmc_att
   return LLMC_OK;
 }
 
+// Rows of `bytes` bytes, `ld` bytes apart.
+struct Rows { uintptr_t at; size_t n, bytes, ld; };
+// whether some row of a has a byte in [lo, hi)
+static bool meets(const Rows& a, uintptr_t lo, uintptr_t hi) {
+  if (a.n == 0 || lo >= hi || a.at >= hi) return false;
+  const size_t first = lo < a.at + a.bytes ? 0 : (lo - a.at - a.bytes) / a.ld + 1;     // the first row that ends behind lo
+  return first < a.n && a.at + first * a.ld < hi;
+}
+// whether rows of a and of b share a byte (rows of one buffer may lie between each other)
+static bool meets(const Rows& a, const Rows& b) {
+  if (a.n == 0 || b.n == 0) return false;
+  if (!meets(Rows{a.at, 1, (a.n - 1) * a.ld + a.bytes, 1}, b.at, b.at + (b.n - 1) * b.ld + b.bytes)) return false;
+  if (a.ld == b.ld) {
+    const size_t off = a.at < b.at ? (b.at - a.at) % a.ld : (a.ld - (a.at - b.at) % a.ld) % a.ld;       // b's row behind a's
+    return off < a.bytes || a.ld - off < b.bytes;
+  }
+  for (size_t i = 0; i < a.n; ++i)
+    if (meets(b, a.at + i * a.ld, a.at + i * a.ld + a.bytes)) return true;
+  return false;
+}
+static bool meets_pages(const llmc_kv_desc_t* kv, const Rows& a) {
+  const size_t bytes = (size_t)kv->n_pages * kv->n_kv_heads * kv->page_size * kv->head_dim * elem_size(kv->dtype);
+  return meets(a, (uintptr_t)kv->d_k, (uintptr_t)kv->d_k + bytes) || meets(a, (uintptr_t)kv->d_v, (uintptr_t)kv->d_v + bytes);
+}
+
 llmc_status_t llmc_kv_append(const llmc_kv_desc_t* kv, const llmc_kv_batch_t* batch, const void* d_k_new, int64_t ld_k,
                              const void* d_v_new, int64_t ld_v, const int32_t* d_pos_new, llmc_stream_t stream) {
   LLMC_TRY(check_kv(kv, false));
@@ -518,7 +543,6 @@ llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch
   LLMC_TRY(check_attn(kv, batch, attn));
   LLMC_TRY(check_attn_values(batch, attn));
   REQUIRE((d_q && d_out) || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "queries or outputs are NULL");
-  REQUIRE(d_q != d_out || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "d_q and d_out must not overlap");
   const int64_t row = (int64_t)attn->n_heads * kv->head_dim, per = 16 / (int64_t)elem_size(kv->dtype);
   REQUIRE(ld_q >= row && ld_out >= row && ld_q % per == 0 && ld_out % per == 0, LLMC_ERR_SHAPE,
           "row strides must be at least n_heads * head_dim and multiples of 16 bytes");
@@ -527,6 +551,10 @@ llmc_status_t llmc_attention_paged(const llmc_kv_desc_t* kv, const llmc_kv_batch
   const size_t need = attention_paged_ws_bytes(kv->dtype, kv->head_dim, kv->n_kv_heads, attn->n_heads, batch->n_rows,
                                                batch->n_seqs, batch->max_new, batch->max_len, attn->accumulate == 1);
   REQUIRE(d_workspace && workspace_bytes >= need, LLMC_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  const size_t e = elem_size(kv->dtype);
+  const Rows in = {(uintptr_t)d_q, (size_t)batch->n_rows, row * e, ld_q * e}, out = {(uintptr_t)d_out, in.n, in.bytes, ld_out * e};
+  REQUIRE(!meets(in, out), LLMC_ERR_INVALID_ARG, "d_q and d_out must not overlap");
+  REQUIRE(!meets_pages(kv, out), LLMC_ERR_INVALID_ARG, "d_out must not overlap the pages");
   return launch_attention_paged(kv, batch, attn, d_q, ld_q, d_out, ld_out, d_workspace, (hipStream_t)stream);
 }
 
@@ -577,12 +605,15 @@ llmc_status_t llmc_layer_forward_paged(const llmc_layer_desc_t* layer, const llm
   REQUIRE(kv->n_kv_heads == layer->n_heads && attn->n_heads == layer->n_heads && kv->head_dim == 64, LLMC_ERR_SHAPE,
           "the cache's heads do not fit the layer's");
   REQUIRE((d_h_in && d_h_out) || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "d_h_in/d_h_out is NULL");
-  REQUIRE(d_h_in != d_h_out || batch->n_rows == 0, LLMC_ERR_INVALID_ARG, "d_h_in and d_h_out must not overlap");
   REQUIRE(aligned16(d_h_in) && aligned16(d_h_out), LLMC_ERR_SHAPE, "d_h_in and d_h_out must be 16-byte aligned");
   REQUIRE(((uintptr_t)d_workspace & 255) == 0, LLMC_ERR_SHAPE, "the workspace must be 256-byte aligned");
   const size_t need = layer_paged_ws_bytes(layer, batch->n_rows, batch->n_seqs, batch->max_new, batch->max_len,
                                            attn->accumulate == 1);
   REQUIRE(d_workspace && workspace_bytes >= need, LLMC_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  const size_t bytes = batch->n_rows * (size_t)layer->d * elem_size(layer->dtype);
+  const Rows out = {(uintptr_t)d_h_out, batch->n_rows > 0, bytes, bytes};
+  REQUIRE(!meets(out, (uintptr_t)d_h_in, (uintptr_t)d_h_in + bytes), LLMC_ERR_INVALID_ARG, "d_h_in and d_h_out must not overlap");
+  REQUIRE(!meets_pages(kv, out), LLMC_ERR_INVALID_ARG, "d_h_out must not overlap the pages");
   return launch_layer_paged(layer, kv, batch, attn, d_pos_new, d_h_in, d_h_out, d_workspace, (hipStream_t)stream);
 }
 

@@ -259,3 +259,37 @@ def test_weights_of_slots_beyond_one_dimension(L):
     c.check(out.cpu())
     weight[at] = 3.0
     assert (weight == 3.0).all()
+
+
+@pytest.mark.parametrize("first,second,ld", [(0, 4, 9), (5, 0, 9), (1, 5, 16), (0, 4, 8), (4, 0, 8)])
+def test_queries_and_outputs_between_each_other_in_one_buffer(L, first, second, ld):
+    """Rows of outputs that lie between the rows of queries overlap nothing."""
+    c = Case(L, "bf16", 4, 2, 64, 16, [90, 200, 33], [20, 40, 33], seed=8)
+    want = c.gpu()
+    wide = torch.full((c.q.shape[0] + 1, ld, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    n = c.q.shape[0]
+    q, out = wide[:n, first:first + 4], wide[1:, second:second + 4] if second < first else wide[:n, second:second + 4]
+    q.copy_(c.q.cuda())
+    kp, vp, tab = c.k.cuda(), c.v.cuda(), c.table.cuda()
+    ws = torch.empty((L.llmc_attention_paged_workspace_bytes(q, kp, tab, max_new=c.max_new, max_len=c.max_len),), dtype=torch.uint8,
+                     device="cuda")
+    L.llmc_attention_paged(q, kp, vp, tab, i32(c.lens), out, ws, new_start=i32(c.starts), max_new=c.max_new, max_len=c.max_len)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), want) and torch.equal(q.cpu(), c.q)
+    with pytest.raises(L.LlmcError, match="overlap"):
+        L.llmc_attention_paged(q, kp, vp, tab, i32(c.lens), wide[:n, first + 1:first + 5] if first + 5 <= ld else wide[:n, first - 1:first + 3],
+                               ws, new_start=i32(c.starts), max_new=c.max_new, max_len=c.max_len)
+
+
+def test_queries_and_outputs_of_other_strides_in_one_buffer(L):
+    """Two rows of queries 1024 elements apart, two of outputs 512 apart, the first behind the first: next to each other, not over."""
+    c = Case(L, "bf16", 4, 2, 64, 16, [90, 20], [1, 1], seed=9)
+    want = c.gpu(decode=True)
+    flat = torch.full((2400,), 3.0, dtype=torch.bfloat16, device="cuda")
+    q, out = flat.as_strided((2, 4, 64), (1024, 64, 1), 0), flat.as_strided((2, 4, 64), (512, 64, 1), 256)
+    q.copy_(c.q.cuda())
+    kp, vp, tab = c.k.cuda(), c.v.cuda(), c.table.cuda()
+    ws = torch.empty((L.llmc_attention_paged_workspace_bytes(q, kp, tab, max_len=c.max_len),), dtype=torch.uint8, device="cuda")
+    L.llmc_attention_paged(q, kp, vp, tab, i32(c.lens), out, ws, max_len=c.max_len)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), want) and torch.equal(q.cpu(), c.q)
