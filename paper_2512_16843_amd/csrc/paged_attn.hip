@@ -839,7 +839,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
   const int slots = a.p.max_pages << a.p.page_shift;
   const int32_t* pos = FEAT == 2 ? a.pos + (size_t)rb.b * slots : nullptr;
   // keys below this slot are out of the window of some row of the wavefront
-  const int w_first = FEAT == 2 || a.window <= 0 ? INT32_MIN : t_last - a.window + 1;
+  const int w_first = FEAT == 2 || a.window <= 0 ? INT32_MIN : (int)max((int64_t)t_last - a.window + 1, (int64_t)INT32_MIN);
 
   const uint16_t* qp = (const uint16_t*)a.q + (size_t)row * a.ld_q + head * DH;
   bf16x8_t fq[KS];
