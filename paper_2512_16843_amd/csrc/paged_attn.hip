@@ -1356,6 +1356,11 @@ struct Plan {
 // How a call is cut.  Up to 16 rows a head (single tokens above all): 16-row products with the keys dealt to wavefronts.  More
 // rows in bf16 share key tiles in LDS, in fp32 (bound by the matrix instructions of that type) 64 rows walk the keys together.
 // The key axis is cut where there are too few row blocks to fill the chip.
+// The line at 16 rows is what one product of a wavefront holds.  In bf16 the tiles would be slower below it where the call is short (one sequence
+// of 1000 tokens, 12 heads of 64, 8 and 16 new ones: 8.9 and 9.5 us, in tiles 14.4 and 14.0; 64 sequences of up to 300, 8 and 16 new:
+// 14.1 and 15.7, in tiles 13.9 and 14.6) and faster where it is long (16 of up to 2048, 8 and 16 new: 27.6 and 29.0, in tiles 24.5 and
+// 23.7; 4 of up to 8192, 8 heads of 128 shared by four each, 2 and 4 new: 37 and 42, in tiles 32 and 33), but they round weights to 8 bits for
+// 16, and the weights of cached tokens would take a second pass over the keys.
 // span: the longest range of keys that a row block can see (a window may make it shorter than max_len); workspaces are sized
 // for span = max_len, and a shorter one never gets more pieces.
 Plan make_plan(int dtype, int head_dim, int n_rows, int n_seqs, int n_kv, int G, int max_new, int max_len, int span) {
