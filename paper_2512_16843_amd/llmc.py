@@ -652,6 +652,9 @@ def llmc_layer_forward_paged(layer: Layer, h_in: torch.Tensor, h_out: torch.Tens
     dev = k_pages.get_device()
     kd = _kv_desc(k_pages, v_pages, dev)
     n = h_in.shape[0]
+    for name, t in layer.w.items():
+        if t.get_device() != dev:
+            _refuse(ERR_INVALID_ARG, "the layer's %s is on %s, the pages are on device %d" % (name, t.device, dev))
     bd = _kv_batch(kd.page_size, dev, table, length, new_start, n, max_new, max_len, pos, weight)
     H = layer.n_heads
     ad = AttnDesc(H, kd.head_dim ** -0.5, softcap, window,

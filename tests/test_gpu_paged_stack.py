@@ -241,3 +241,17 @@ def test_the_block_with_scores_that_are_not_plain(L, dtype, opts, news):
     for b in range(2):
         rtol = 1e-4 if dtype == "f32" else 0.1
         assert np.allclose(weight[b, :at[b]].cpu().numpy(), [c[1] for c in plain[b].cache], rtol=rtol, atol=1e-5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["wqkv", "ln2_b"])
+def test_a_layer_whose_weights_lie_elsewhere_is_refused(L, name):
+    _, cfg, ws = small_decoder("f32", n_layers=1)
+    layer = L.layer_from_weights(cfg, ws[0], "cuda")
+    layer.w[name] = layer.w[name].cpu()
+    k = torch.zeros((2, cfg.n_heads, 16, 64), device="cuda")
+    h = torch.zeros((1, cfg.d), device="cuda")
+    ws_ = torch.empty((L.llmc_layer_paged_workspace_bytes(layer, 1, 1, 1, 16),), dtype=torch.uint8, device="cuda")
+    with pytest.raises(L.LlmcError, match=name) as e:
+        L.llmc_layer_forward_paged(layer, h, torch.empty_like(h), k, k.clone(), i32([[0]]), i32([1]), ws_)
+    assert e.value.status == L.ERR_INVALID_ARG
