@@ -182,8 +182,9 @@ class PagedStack:
     ``extend`` computes the new tokens only (a prompt, a chunk of one, or one token of each sequence; any mix).
 
     Pages are handed out by the host from one free list (so ``extend`` is not for capture in a graph; the library's calls below it
-    are); all layers share the page table and the lengths, each has its own pools.  ``budget`` (with its protected ``sink`` first positions and ``recent`` last ones): after each ``extend`` every
-    layer keeps that many tokens of a sequence, those that have gathered the largest attention weight in that layer."""
+    are); all layers share the page table and the lengths, each has its own pools.  ``budget`` (with its protected ``sink`` first
+    positions and ``recent`` last ones): after each ``extend`` every layer keeps that many tokens of a sequence, those that have
+    gathered the largest attention weight in that layer."""
 
     def __init__(self, cfg: ModelConfig, weights, n_seqs: int, max_len: int, n_pages: Optional[int] = None,
                  page_size: int = 16, device="cuda", budget: int = 0, sink: int = 4, recent: int = 32, window: int = 0):
@@ -191,7 +192,7 @@ class PagedStack:
             raise ValueError("only a causal decoder has a key/value cache")
         if budget and not 0 < budget <= max_len:
             raise ValueError("the budget must lie between 1 and max_len")
-        self.cfg, self.device, self.n_seqs, self.page, self.max_len = cfg, device, n_seqs, page_size, max_len
+        self.cfg, self.n_seqs, self.page, self.max_len = cfg, n_seqs, page_size, max_len
         self.budget, self.sink, self.recent, self.window = budget, sink, recent, window
         self.layers = [llmc.layer_from_weights(cfg, w, device) for w in weights]
         self.max_pages = (max_len + page_size - 1) // page_size
@@ -208,6 +209,7 @@ class PagedStack:
         self.lengths = [0] * n_seqs           # tokens in the cache
         self.next_pos = [0] * n_seqs          # tokens ever seen: the position of the next one
         self.workspace = torch.empty((0,), dtype=torch.uint8, device=device)
+        self.device = self.workspace.device   # "cuda" is the device that is current now, whichever is at a later call
 
     def extend(self, h: torch.Tensor, new: List[int]) -> torch.Tensor:
         """``h`` [sum(new), d]: the embedded new tokens, ``new[b]`` of them for sequence b, in order.  Returns their outputs.

@@ -255,3 +255,11 @@ def test_a_layer_whose_weights_lie_elsewhere_is_refused(L, name):
     with pytest.raises(L.LlmcError, match=name) as e:
         L.llmc_layer_forward_paged(layer, h, torch.empty_like(h), k, k.clone(), i32([[0]]), i32([1]), ws_)
     assert e.value.status == L.ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_a_stack_stays_on_the_device_it_was_made_on(L):
+    from paper_2512_16843_amd.engine import PagedStack
+    _, cfg, ws = small_decoder("f32", n_layers=1)
+    st = PagedStack(cfg, ws, 1, 32)
+    assert st.device == torch.device("cuda", torch.cuda.current_device()) == st.k[0].device
