@@ -366,8 +366,9 @@ static llmc_status_t layer_t(const llmc_layer_desc_t* L, const void* h_in, void*
 }
 
 // ---- the decoder block on new tokens over a paged cache -------------------------------------------------
-// The same launches on n_rows rows, with the attention over whole sequences replaced by storing the new keys and values
-// and attending over the pages.
+// The same products and LayerNorms on n_rows rows, with the attention over whole sequences replaced by storing the new keys
+// and values and attending over the pages.  The products do not read the weights of those that follow ahead, as the whole
+// sequences' block has them do.
 size_t layer_paged_ws_bytes(const llmc_layer_desc_t* L, int n_rows, int n_seqs, int max_new, int max_len, bool weights) {
   return layer_ws_bytes(L, 1, n_rows) + align_up(attention_paged_ws_bytes(L->dtype, 64, L->n_heads, L->n_heads, n_rows, n_seqs, max_new,
                                                                           max_len, weights), 256);
