@@ -21,7 +21,9 @@ namespace {
 typedef const __attribute__((address_space(4))) int32_t scalar_i32;    // read through the scalar cache
 constexpr float kLog2e = 1.4426950408889634f;
 // The maximum that a row's sums count from follows its scores only where they outgrow it by this much in base 2: weights up to
-// 2^8 are as good as weights up to one in floating point, and most steps then rescale nothing.
+// 2^8 are as good as weights up to one in floating point, and most steps then rescale nothing.  (Where weights are rounded to bf16 the largest
+// is then not exactly one: chunks in tiles 2.4e-4 from the exact result on average, 2.2e-4 without the slack, and 2 to 6 % slower: 16
+// prompts of 1024 tokens 49.9 and 50.9 us, a chunk of 512 over 16384 tokens, 32 heads of 128, 200 and 208.)
 constexpr float kSlack = 8.f;
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
@@ -636,7 +638,7 @@ __global__ __launch_bounds__(256) void attention_paged_rows_kernel(AttnArgs a) {
   for (; __builtin_expect(again != 0, 0); again &= again - 1) {
     const int col = __builtin_ctz(again), mr = m0 + col;
     const auto of_row = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), col)); };
-    const float ref = of_row(m_run), sc = of_row(scale);
+    const float ref = of_row(m_run) == -INFINITY ? 0.f : of_row(m_run), sc = of_row(scale);
     const int i = token_of(a, mr), r = s.first + i, hd = h * a.G + mr - i * a.G;
     float* part = whole ? nullptr : ROWSPLIT ? a.part_o + (((size_t)r * a.H + hd) * a.n_split + piece) * DH : rows_lds + (wave * R + col) * LDO;
     sum_seen<T, DH, false>(a, rb, h, mr, ref, k_first, k_hi, STEP, KEYS, part, (T*)a.out + (size_t)r * a.ld_out + hd * DH, sc);
@@ -1097,7 +1099,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : FEAT ? 3 : 4) void attention_p
   for (; __builtin_expect(again != 0, 0); again &= again - 1) {
     const int col = __builtin_ctz(again), mr = m0 + col;
     const auto of_row = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), col)); };
-    const float ref = of_row(m_run), sc = of_row(scale);
+    const float ref = of_row(m_run) == -INFINITY ? 0.f : of_row(m_run), sc = of_row(scale);
     const int i = token_of(a, mr), r = s.first + i, hd = h * a.G + mr - i * a.G;
     float* part = whole ? nullptr : a.part_o + (((size_t)r * a.H + hd) * a.n_split + piece) * DH;
     sum_seen<bf16_t, DH, FEAT == 0>(a, rb, h, mr, ref, k_lo, k_hi, 64, 64, part, (bf16_t*)a.out + (size_t)r * a.ld_out + hd * DH, sc);
