@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // narrowed by digits of 11 bits, most significant first, a histogram in LDS a digit, until at most 64 keys share the digits
 // so far (two digits, as weights go); a wavefront then ranks those by key and slot.  Holes and movers are numbered by counts
 // of ballots.  Up to 24576 tokens the keys are read once and stay in registers.  Bound: latency, one workgroup's chain of loads and
-// barriers (64 sequences of 1040 tokens 8.6 us, 8 of up to 8192 14; eight digits of 8 bits and keys read in each pass 17.4 and 42).
+// barriers (64 sequences of 1040 tokens 8.6 us, 8 of up to 8192 14.5; eight digits of 8 bits and keys read in each pass 17.4 and 42).
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kDigit = 11, kBins = 1 << kDigit;
 
 struct EvictArgs {
