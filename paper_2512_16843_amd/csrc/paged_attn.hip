@@ -137,7 +137,8 @@ struct Item { int b, mb, piece; SeqRange s; };      // b < 0: nothing
 // hidden, and zero times an infinity or a NaN is no zero.  Where a row's output is not finite although its normaliser is, the values of
 // the keys that are hidden from some row of the wavefront are looked at; if one of those is not finite, the row is summed again,
 // over what it sees and nothing else.  That is far slower; where all is finite it costs the test of the outputs, which no time
-// shows.  (Infinities in the first token of 16 prompts of 1024 tokens, 12 heads: 5 ms if every row that sees them is summed again.)
+// shows.  (An infinity in the first token of each of 16 prompts of 1024 tokens, 12 heads of 64, 48 us without it: 61 us this way, 5 ms if
+// every row that sees it were summed again.)
 
 // whether a value of a key hidden from some of the rows with slots t_first to t_last is not finite, of keys [lo, hi) and those behind
 // that share their last step
